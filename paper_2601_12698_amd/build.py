@@ -122,6 +122,30 @@ def build_native(force: bool) -> None:
         warnings.warn(f"the module _native is not built, and calls from Python take some 2 us longer: {e}")
 
 
+def _compile_serving(force: bool, jobs: int, hdrs) -> list:
+    """Objects of the operators around a decode step's attention.  The attention kernels are one unit for each element type,
+    cache format and padded head size, so that they compile side by side."""
+    deps = [*hdrs, os.path.join(CSRC, "serving_internal.h"), *(os.path.join(ROOT, "include", h) for h in ("rotary.h", "kvcache.h", "prefixattn.h"))]
+    attn = [os.path.join(CSRC, "prefixattn_kernel.h"), os.path.join(CSRC, "prefixattn_args.h")]
+    units = [(n, n[:-4], [], []) for n in ("rotary.hip", "kvcache.hip")] + [("prefixattn.hip", "prefixattn", [], attn)]
+    for dt in (0, 1):
+        for fmt in (0, 1):
+            for dp in (64, 128, 256):
+                units.append(("prefixattn_unit.hip", f"prefixattn_d{dt}_f{fmt}_h{dp}", [f"-DUNIT_DT={dt}", f"-DUNIT_FORMAT={fmt}", f"-DUNIT_DP={dp}"], attn))
+
+    def one(unit):
+        src, name, defs, more = os.path.join(CSRC, unit[0]), unit[1], unit[2], unit[3]
+        obj = os.path.join(BUILD, name + ".o")
+        if force or not _newer(obj, src, *deps, *more):
+            r = _run(["hipcc", *DEVICE_FLAGS, *INCLUDES, *defs, "-Rpass-analysis=kernel-resource-usage", "-c", src, "-o", obj])
+            with open(obj[:-2] + ".remarks", "w") as f:
+                f.write(r.stderr)
+        return obj
+
+    with cf.ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
+        return list(ex.map(one, units))
+
+
 def build(force: bool = False, jobs: int = 8, verbose: bool = False) -> str:
     sys.path.insert(0, CSRC)
     try:
@@ -171,6 +195,7 @@ def build(force: bool = False, jobs: int = 8, verbose: bool = False) -> str:
             with open(obj[:-2] + ".remarks", "w") as f:
                 f.write(r.stderr)
         objs.append(obj)
+    objs += _compile_serving(force, jobs, hdrs)
     tmp = LIB + f".{os.getpid()}.tmp"
     _run(["hipcc", "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs])
     os.replace(tmp, LIB)

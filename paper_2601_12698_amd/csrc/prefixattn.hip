@@ -1,0 +1,200 @@
+// Host side of attention over a shared prefix (include/prefixattn.h): argument checks, how the work is split, and the kernel
+// that joins the splits' results.
+#include <math.h>
+
+#include "prefixattn.h"
+#include "prefixattn_args.h"
+#include "serving_internal.h"
+
+using namespace addrms_host;
+using namespace serving;
+
+namespace {
+
+// out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, lse = ln 2 (m + log2 of that sum), over the parts that were run: a suffix
+// has as many as its length says.  A workgroup joins one row; its threads are columns of four elements by groups of parts.
+template <int DT>
+__global__ __launch_bounds__(kAttnThreads) void join_kernel(const AttnArgs a)
+{
+    typedef typename elem<DT>::type T;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    __shared__ float weight[2 * kMaxSplits], red[2][4];
+    __shared__ f32x4 sums[kAttnThreads];
+    const int32_t row = static_cast<int32_t>(blockIdx.x), tid = static_cast<int32_t>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+    const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
+    int32_t parts = a.prefix_splits;
+    if (a.suffix_splits) {
+        const int32_t keys = min(max(at_global<const int32_t>(a.suffix_lens)[row / (a.q_len * a.q_heads)], 0), a.suffix_width << a.page_shift);
+        parts += (keys + a.suffix_chunk - 1) / a.suffix_chunk;
+    }
+    const float2* ml = at_global<const float2>(a.part_ml);
+    float m = -__builtin_huge_valf();
+    for (int32_t p = tid; p < parts; p += kAttnThreads) m = fmaxf(m, ml[p * rows + row].x);
+#pragma unroll
+    for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    if (lane == 0) red[0][wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    float l = 0.0f;
+    for (int32_t p = tid; p < parts; p += kAttnThreads) {
+        const float2 x = ml[p * rows + row];
+        // a part that saw no key has m = -inf, l = 0 and O = 0 (l is NaN where its scores were)
+        const float w = x.x == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f(x.x - m);
+        weight[p] = w;
+        l += w * x.y;
+    }
+#pragma unroll
+    for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+    if (lane == 0) red[1][wave] = l;
+    __syncthreads();
+    l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    const int32_t cols = a.d / 4, groups = kAttnThreads / cols, grp = tid / cols, col = tid - grp * cols;
+    f32x4 x = {0, 0, 0, 0};
+    if (grp < groups)
+        for (int32_t p = grp; p < parts; p += groups) x += weight[p] * *reinterpret_cast<const f32x4*>(at_global<const float>(a.part_o) + (p * rows + row) * a.d + 4 * col);
+    sums[tid] = x;
+    __syncthreads();
+    if (grp == 0) {
+        for (int32_t g = 1; g < groups; ++g) x += sums[g * cols + col];
+        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;              // no key was seen: zeros
+        T4 y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = static_cast<T>(x[j] * inverse);
+        *reinterpret_cast<T4*>(at_global<T>(a.out) + static_cast<int64_t>(row) * a.d + 4 * col) = y;
+        if (a.lse && col == 0) at_global<float>(a.lse)[row] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    }
+}
+
+constexpr int64_t kMaxBlocks = 1 << 24;      // of 256 threads: a launch has fewer than 2^32
+constexpr int32_t kMinChunk = 256;
+
+int32_t splits_of(int64_t keys, int64_t units, int64_t wanted, int32_t* chunk)
+{
+    int64_t n = (wanted + units - 1) / units;
+    if (n > (keys + kMinChunk - 1) / kMinChunk) n = (keys + kMinChunk - 1) / kMinChunk;
+    if (n > kMaxSplits) n = kMaxSplits;
+    if (n < 1) n = 1;
+    const int64_t each = ((keys + n - 1) / n + kChunkStep - 1) / kChunkStep * kChunkStep;
+    *chunk = static_cast<int32_t>(each);
+    return static_cast<int32_t>((keys + each - 1) / each);
+}
+
+struct Plan {
+    AttnArgs a;
+    int prefix_form, suffix_form, dp;
+    int64_t rows, blocks, bytes;
+};
+
+// Checks a shape and splits its work.  A key range is split until there are two workgroups a CU (three of the form for few rows),
+// in pieces of 256 keys or more; what a suffix may hold at most counts, for its length is known on the device alone.
+int plan_of(const prefixattn_shape* s, Plan* p)
+{
+    if (!s) return fail(ADDRMS_ERR_INVALID_ARG, "shape is NULL");
+    if (s->dtype != ADDRMS_BF16 && s->dtype != ADDRMS_FP16) return fail(ADDRMS_ERR_UNSUPPORTED_DTYPE, "unsupported dtype %d for attention", s->dtype);
+    if (s->format != KVCACHE_SAME && s->format != KVCACHE_E4M3) return fail(ADDRMS_ERR_INVALID_ARG, "unknown cache format %d", s->format);
+    if (s->batch < 0 || s->q_len < 0 || s->q_heads <= 0 || s->kv_heads <= 0 || s->d <= 0 || s->pages < 0 || s->prefix_len < 0 || s->suffix_width < 0)
+        return fail(ADDRMS_ERR_INVALID_ARG, "sizes must not be negative, heads and d must be > 0");
+    if (s->q_heads % s->kv_heads != 0)
+        return fail(ADDRMS_ERR_INVALID_ARG, "q_heads=%d is not a multiple of kv_heads=%d", s->q_heads, s->kv_heads);
+    if (!power_of_two(s->page_size) || s->page_size > 65536)
+        return fail(ADDRMS_ERR_INVALID_ARG, "page_size must be a power of two up to 65536 (got %d)", s->page_size);
+    if (s->d % 16 != 0 || s->d > KVCACHE_MAX_HEAD)
+        return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "d=%d is not a multiple of 16 up to %d", s->d, KVCACHE_MAX_HEAD);
+    const int64_t width = s->suffix_width < (1ll << 30) ? s->suffix_width * s->page_size : 1ll << 30;
+    if (s->pages >= (1ll << 31) || s->prefix_len >= (1ll << 30) || width >= (1ll << 30) || s->q_heads > 65536)
+        return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "pages, keys or heads are beyond the limits (2^31, 2^30, 65536)");
+    *p = Plan{};
+    AttnArgs& a = p->a;
+    a.batch = s->batch, a.q_len = s->q_len, a.q_heads = s->q_heads, a.kv_heads = s->kv_heads, a.group = s->q_heads / s->kv_heads, a.d = s->d;
+    a.page_shift = log2_of(s->page_size), a.pages = static_cast<int32_t>(s->pages);
+    a.prefix_len = static_cast<int32_t>(s->prefix_len), a.suffix_width = static_cast<int32_t>(s->suffix_width);
+    p->dp = s->d <= 64 ? 64 : s->d <= 128 ? 128 : 256;
+    if (s->batch == 0 || s->q_len == 0) return ADDRMS_OK;
+    const int64_t tokens = static_cast<int64_t>(s->batch) * s->q_len;
+    if (tokens > kMaxBlocks || tokens * s->q_heads > kMaxBlocks)
+        return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld queries of %d heads are beyond the limit (2^24 together)", (long long)tokens, s->q_heads);
+    p->rows = tokens * s->q_heads;
+    const int64_t all = tokens * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
+    p->suffix_form = own <= kFewRows ? FEW : MANY;
+    p->prefix_form = all <= kFewRows ? FEW : MANY;
+    auto tiles = [](int64_t rows, int form) { return form == FEW ? (rows + kFewRows - 1) / kFewRows : (rows + kManyRows - 1) / kManyRows; };
+    if (a.prefix_len) {
+        a.prefix_tiles = static_cast<int32_t>(tiles(all, p->prefix_form));
+        a.prefix_splits = splits_of(a.prefix_len, static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, p->prefix_form == FEW ? 768 : 512, &a.prefix_chunk);
+        p->blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
+    } else {
+        p->prefix_form = p->suffix_form;
+    }
+    const int64_t prefix_blocks = p->blocks;
+    if (width) {
+        a.suffix_tiles = static_cast<int32_t>(tiles(own, p->suffix_form));
+        const int64_t units = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads * s->batch;
+        a.suffix_splits = splits_of(width, units, p->suffix_form == FEW ? 768 : 512, &a.suffix_chunk);
+        p->blocks += units * a.suffix_splits;
+    }
+    if (p->blocks > kMaxBlocks) return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)p->blocks);
+    a.prefix_blocks = static_cast<int32_t>(prefix_blocks);
+    const int64_t parts = a.prefix_splits + a.suffix_splits;
+    p->bytes = parts * p->rows * (4ll * a.d + 8);
+    return ADDRMS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t prefixattn_workspace_bytes(const prefixattn_shape* shape)
+{
+    Plan p;
+    if (const int st = plan_of(shape, &p)) return st;
+    return p.bytes;
+}
+
+int64_t prefixattn_algorithmic_bytes(const prefixattn_shape* shape, int64_t suffix_keys)
+{
+    Plan p;
+    if (const int st = plan_of(shape, &p)) return st;
+    if (suffix_keys < 0) return fail(ADDRMS_ERR_INVALID_ARG, "suffix_keys must be >= 0");
+    const int64_t key = 2ll * shape->kv_heads * (shape->format == KVCACHE_E4M3 ? shape->d + 1 : 2 * shape->d);
+    return (shape->prefix_len + suffix_keys) * key + p.rows * (4ll * shape->d + 4);
+}
+
+int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages, const void* v_pages, const uint8_t* k_scale, const uint8_t* v_scale,
+                   const int32_t* prefix_pages, const int32_t* suffix_pages, const int32_t* suffix_lens, void* out, float* lse, float scale,
+                   const prefixattn_shape* shape, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    Plan p;
+    if (const int st = plan_of(shape, &p)) return st;
+    if (!(scale > 0.0f) || !(scale < INFINITY)) return fail(ADDRMS_ERR_INVALID_ARG, "scale must be > 0 and finite (got %g)", static_cast<double>(scale));
+    if (shape->batch == 0 || shape->q_len == 0) return ADDRMS_OK;
+    AttnArgs& a = p.a;
+    const bool codes = shape->format == KVCACHE_E4M3, keys = a.prefix_splits || a.suffix_splits;
+    if (!q || !q_strides || !out || (keys && (!k_pages || !v_pages || !workspace || (codes && (!k_scale || !v_scale)))) ||
+        (a.prefix_splits && !prefix_pages) || (a.suffix_splits && (!suffix_pages || !suffix_lens)))
+        return fail(ADDRMS_ERR_INVALID_ARG, "no pointer may be NULL");
+    if (workspace_bytes < p.bytes)
+        return fail(ADDRMS_ERR_INVALID_ARG, "the workspace has %lld bytes, the call needs %lld", (long long)workspace_bytes, (long long)p.bytes);
+    if (!aligned_to(q, 2) || !aligned_to(out, 16) || !aligned_to(lse, 4) || !aligned_to(k_pages, 16) || !aligned_to(v_pages, 16) ||
+        !aligned_to(workspace, 16) || !aligned_to(prefix_pages, 4) || !aligned_to(suffix_pages, 4) || !aligned_to(suffix_lens, 4))
+        return fail(ADDRMS_ERR_MISALIGNED, "pages, out and workspace must be 16-byte aligned, the others to their elements");
+    a.q = addr(q), a.k_pages = addr(k_pages), a.v_pages = addr(v_pages), a.k_scale = addr(k_scale), a.v_scale = addr(v_scale);
+    a.prefix_pages = addr(prefix_pages), a.suffix_pages = addr(suffix_pages), a.suffix_lens = addr(suffix_lens), a.out = addr(out), a.lse = addr(lse);
+    a.part_o = addr(workspace);
+    a.part_ml = a.part_o + 4ull * (a.prefix_splits + a.suffix_splits) * p.rows * a.d;
+    a.q_token = q_strides[0], a.q_head = q_strides[1];
+    a.c = scale * 1.44269504088896340736f;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (p.blocks) {
+        static constexpr AttnLaunch kUnits[2][2][3] = {
+            {{ATTN_UNIT(0, 0, 64), ATTN_UNIT(0, 0, 128), ATTN_UNIT(0, 0, 256)}, {ATTN_UNIT(0, 1, 64), ATTN_UNIT(0, 1, 128), ATTN_UNIT(0, 1, 256)}},
+            {{ATTN_UNIT(1, 0, 64), ATTN_UNIT(1, 0, 128), ATTN_UNIT(1, 0, 256)}, {ATTN_UNIT(1, 1, 64), ATTN_UNIT(1, 1, 128), ATTN_UNIT(1, 1, 256)}}};
+        const AttnLaunch unit = kUnits[shape->dtype == ADDRMS_FP16][codes][p.dp == 64 ? 0 : p.dp == 128 ? 1 : 2];
+        SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.blocks), s));
+    }
+    if (shape->dtype == ADDRMS_FP16) join_kernel<DT_FP16><<<static_cast<unsigned>(p.rows), kAttnThreads, 0, s>>>(a);
+    else join_kernel<DT_BF16><<<static_cast<unsigned>(p.rows), kAttnThreads, 0, s>>>(a);
+    SERVING_HIP_TRY(hipGetLastError());
+    return ADDRMS_OK;
+}
+
+}  // extern "C"
