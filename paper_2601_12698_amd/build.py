@@ -100,14 +100,14 @@ def _compile_native(force: bool) -> None:
     from .binding import torch_identity
     tdir, identity = os.path.dirname(torch.__file__), torch_identity()
     src, obj = os.path.join(CSRC, "native_calls.cpp"), os.path.join(BUILD, "native_calls.cpp.o")
-    if not force and _newer(NATIVE, src):
+    if not force and _newer(NATIVE, src, *(os.path.join(ROOT, "include", h) for h in ("addrms.h", "rotary.h", "kvcache.h", "prefixattn.h"))):
         with open(NATIVE, "rb") as f:
             if identity.encode() in f.read():
                 return
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
     inc = [os.path.join(tdir, "include"), os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
            os.path.join(rocm, "include"), sysconfig.get_paths()["include"]]
-    _run(["g++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+    _run(["g++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I", os.path.join(ROOT, "include"), f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
           f'-DTORCH_IDENTITY="{identity}"', *(a for i in inc for a in ("-isystem", i)), "-c", src, "-o", obj])
     tmp = NATIVE + f".{os.getpid()}.tmp"
     _run(["g++", "-shared", "-o", tmp, obj, "-L", os.path.join(tdir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"])

@@ -49,6 +49,20 @@ SIGNATURES = {
 }
 
 _lib = None
+_bound = None           # the module _native that these entry points were handed to
+
+
+def _fast():
+    """Module _native, which takes the usual calls as one native call (csrc/native_calls.cpp), or None."""
+    global _bound
+    native = B._native
+    if native is not _bound:
+        if native is not None:
+            lib = load()
+            native.bind_serving(B.DTYPE_IDS, *(ctypes.cast(getattr(lib, f), c_void_p).value for f in
+                                               ("rotary_run", "kvcache_write", "kvcache_read", "prefixattn_run")))
+        _bound = native
+    return native
 
 
 def load() -> ctypes.CDLL:
@@ -154,6 +168,12 @@ def rotary_run(q, k, q_out, k_out, positions, inv_freq, pair_axis, dtype, interl
                stream=None) -> None:
     """Turns q [tokens, q_heads, d] and k [tokens, k_heads, d] (None: queries alone) by their positions [axes, tokens] (int64);
     ``inverse`` turns back, which is the gradient.  q_out and k_out may be q and k themselves."""
+    if stream is None and (B._torch_facts or B._torch()) and (native := _fast()) is not None:
+        st = native.rotary_run(q, k, q_out, k_out, positions, inv_freq, pair_axis, dtype, interleaved, inverse)
+        if st is not None:
+            if st:
+                B._check(st)
+            return
     dt = _dtype(dtype, (B.BF16, B.FP16, B.FP32))
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out are given together")
@@ -186,6 +206,12 @@ def kvcache_algorithmic_bytes(tokens: int, heads: int, d: int, dtype, quantised:
 def kvcache_write(k, v, slots, k_pages, v_pages, k_scale, v_scale, dtype, stream=None) -> None:
     """Tokens k, v [tokens, heads, d] go to their slots (int64 [tokens]) of the pages [pages, heads, page_size, d]: quantised
     where the pages are ``float8_e4m3fn`` (or bytes) with scale bytes [pages, heads, page_size], else copied (scales None)."""
+    if stream is None and (B._torch_facts or B._torch()) and (native := _fast()) is not None:
+        st = native.kvcache_write(k, v, slots, k_pages, v_pages, k_scale, v_scale, dtype)
+        if st is not None:
+            if st:
+                B._check(st)
+            return
     dt = _dtype(dtype)
     fmt, pages, heads, page, d, ptrs = _cache(k_pages, v_pages, k_scale, v_scale, dt, k.device)
     if k.dim() != 3:
@@ -198,6 +224,12 @@ def kvcache_write(k, v, slots, k_pages, v_pages, k_scale, v_scale, dtype, stream
 
 def kvcache_read(k_pages, v_pages, k_scale, v_scale, slots, k_out, v_out, dtype, stream=None) -> None:
     """Tokens at the slots, back in 16 bits: k_out, v_out [tokens, heads, d], contiguous; zeros for slots outside the cache."""
+    if stream is None and (B._torch_facts or B._torch()) and (native := _fast()) is not None:
+        st = native.kvcache_read(k_pages, v_pages, k_scale, v_scale, slots, k_out, v_out, dtype)
+        if st is not None:
+            if st:
+                B._check(st)
+            return
     dt = _dtype(dtype)
     fmt, pages, heads, page, d, ptrs = _cache(k_pages, v_pages, k_scale, v_scale, dt, slots.device)
     tokens = slots.shape[0]
@@ -229,6 +261,13 @@ def prefixattn_run(q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_l
     ``suffix_lens`` (int32 [batch]) keys in ``suffix_pages`` (int32 [batch, width]) of each sequence; out as q, contiguous, lse
     fp32 [batch * q_len, q_heads] or None.  ``workspace``: bytes on the device, as many as prefixattn_workspace_bytes says; without
     one the call takes it from torch's allocator, on the current stream."""
+    if stream is None and (B._torch_facts or B._torch()) and (native := _fast()) is not None:
+        st = native.prefixattn_run(q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_len, suffix_pages, suffix_lens, out, lse, scale,
+                                   dtype, q_len, workspace)
+        if st is not None:
+            if st:
+                B._check(st)
+            return
     dt = _dtype(dtype)
     if q.dim() != 3 or q_len < 1 or q.shape[0] % q_len:
         raise ValueError(f"q must be [batch * q_len, heads, d], and q_len={q_len} at least 1")
