@@ -14,12 +14,12 @@ namespace {
 // out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, lse = ln 2 (m + log2 of that sum), over the parts that were run: a suffix
 // has as many as its length says.  A workgroup joins one row; its threads are columns of four elements by groups of parts.
 template <int DT>
-__global__ __launch_bounds__(kAttnThreads) void join_kernel(const AttnArgs a)
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttnArgs a)
 {
     typedef typename elem<DT>::type T;
     typedef T T4 __attribute__((ext_vector_type(4)));
     __shared__ float weight[2 * kMaxSplits], red[2][4];
-    __shared__ f32x4 sums[kAttnThreads];
+    __shared__ f32x4 sums[kJoinThreads];
     const int32_t row = static_cast<int32_t>(blockIdx.x), tid = static_cast<int32_t>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
     const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
     int32_t parts = a.prefix_splits;
@@ -29,14 +29,14 @@ __global__ __launch_bounds__(kAttnThreads) void join_kernel(const AttnArgs a)
     }
     const float2* ml = at_global<const float2>(a.part_ml);
     float m = -__builtin_huge_valf();
-    for (int32_t p = tid; p < parts; p += kAttnThreads) m = fmaxf(m, ml[p * rows + row].x);
+    for (int32_t p = tid; p < parts; p += kJoinThreads) m = fmaxf(m, ml[p * rows + row].x);
 #pragma unroll
     for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
     if (lane == 0) red[0][wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
     float l = 0.0f;
-    for (int32_t p = tid; p < parts; p += kAttnThreads) {
+    for (int32_t p = tid; p < parts; p += kJoinThreads) {
         const float2 x = ml[p * rows + row];
         // a part that saw no key has m = -inf, l = 0 and O = 0 (l is NaN where its scores were)
         const float w = x.x == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f(x.x - m);
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kAttnThreads) void join_kernel(const AttnArgs a)
     if (lane == 0) red[1][wave] = l;
     __syncthreads();
     l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-    const int32_t cols = a.d / 4, groups = kAttnThreads / cols, grp = tid / cols, col = tid - grp * cols;
+    const int32_t cols = a.d / 4, groups = kJoinThreads / cols, grp = tid / cols, col = tid - grp * cols;
     f32x4 x = {0, 0, 0, 0};
     if (grp < groups)
         for (int32_t p = grp; p < parts; p += groups) x += weight[p] * *reinterpret_cast<const f32x4*>(at_global<const float>(a.part_o) + (p * rows + row) * a.d + 4 * col);
@@ -103,11 +103,14 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     const int64_t width = s->suffix_width < (1ll << 30) ? s->suffix_width * s->page_size : 1ll << 30;
     if (s->pages >= (1ll << 31) || s->prefix_len >= (1ll << 30) || width >= (1ll << 30) || s->q_heads > 65536)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "pages, keys or heads are beyond the limits (2^31, 2^30, 65536)");
+    const int64_t page_rows = static_cast<int64_t>(s->page_size) * s->kv_heads, row_bytes = s->d * (s->format == KVCACHE_E4M3 ? 1 : 2);
+    if (page_rows * row_bytes >= (1ll << 32)) return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "a page of %lld bytes is beyond the limit (2^32)", (long long)(page_rows * row_bytes));
     *p = Plan{};
     AttnArgs& a = p->a;
     a.batch = s->batch, a.q_len = s->q_len, a.q_heads = s->q_heads, a.kv_heads = s->kv_heads, a.group = s->q_heads / s->kv_heads, a.d = s->d;
     a.page_shift = log2_of(s->page_size), a.pages = static_cast<int32_t>(s->pages);
     a.prefix_len = static_cast<int32_t>(s->prefix_len), a.suffix_width = static_cast<int32_t>(s->suffix_width);
+    a.page_rows = static_cast<uint64_t>(page_rows), a.page_bytes = static_cast<uint64_t>(page_rows * row_bytes);
     p->dp = s->d <= 64 ? 64 : s->d <= 128 ? 128 : 256;
     if (s->batch == 0 || s->q_len == 0) return ADDRMS_OK;
     const int64_t tokens = static_cast<int64_t>(s->batch) * s->q_len;
@@ -115,10 +118,12 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld queries of %d heads are beyond the limit (2^24 together)", (long long)tokens, s->q_heads);
     p->rows = tokens * s->q_heads;
     const int64_t all = tokens * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
-    p->suffix_form = own <= kFewRows ? FEW : MANY;
-    p->prefix_form = all <= kFewRows ? FEW : MANY;
-    auto tiles = [](int64_t rows, int form) { return form == FEW ? (rows + kFewRows - 1) / kFewRows : (rows + kManyRows - 1) / kManyRows; };
-    if (a.prefix_len) {
+    auto form_of = [](int64_t rows) { return rows <= 16 ? FEW : rows <= 64 ? MANY_64 : MANY_128; };
+    auto tiles = [](int64_t rows, int form) { return (rows + kFormRows[form] - 1) / kFormRows[form]; };
+    p->suffix_form = form_of(own);
+    p->prefix_form = form_of(all);
+    // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
+    if (a.prefix_len && a.pages) {
         a.prefix_tiles = static_cast<int32_t>(tiles(all, p->prefix_form));
         a.prefix_splits = splits_of(a.prefix_len, static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, p->prefix_form == FEW ? 768 : 512, &a.prefix_chunk);
         p->blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
@@ -126,7 +131,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         p->prefix_form = p->suffix_form;
     }
     const int64_t prefix_blocks = p->blocks;
-    if (width) {
+    if (width && a.pages) {
         a.suffix_tiles = static_cast<int32_t>(tiles(own, p->suffix_form));
         const int64_t units = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads * s->batch;
         a.suffix_splits = splits_of(width, units, p->suffix_form == FEW ? 768 : 512, &a.suffix_chunk);
@@ -182,6 +187,7 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
     a.part_o = addr(workspace);
     a.part_ml = a.part_o + 4ull * (a.prefix_splits + a.suffix_splits) * p.rows * a.d;
     a.q_token = q_strides[0], a.q_head = q_strides[1];
+    a.q_wide = (a.q | static_cast<uint64_t>(q_strides[0] * 2) | static_cast<uint64_t>(q_strides[1] * 2)) % 16 == 0;
     a.c = scale * 1.44269504088896340736f;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (p.blocks) {
@@ -191,8 +197,8 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
         const AttnLaunch unit = kUnits[shape->dtype == ADDRMS_FP16][codes][p.dp == 64 ? 0 : p.dp == 128 ? 1 : 2];
         SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.blocks), s));
     }
-    if (shape->dtype == ADDRMS_FP16) join_kernel<DT_FP16><<<static_cast<unsigned>(p.rows), kAttnThreads, 0, s>>>(a);
-    else join_kernel<DT_BF16><<<static_cast<unsigned>(p.rows), kAttnThreads, 0, s>>>(a);
+    if (shape->dtype == ADDRMS_FP16) join_kernel<DT_FP16><<<static_cast<unsigned>(p.rows), kJoinThreads, 0, s>>>(a);
+    else join_kernel<DT_BF16><<<static_cast<unsigned>(p.rows), kJoinThreads, 0, s>>>(a);
     SERVING_HIP_TRY(hipGetLastError());
     return ADDRMS_OK;
 }

@@ -13,12 +13,15 @@ struct AttnArgs {
     int32_t batch, q_len, q_heads, kv_heads, group, d, page_shift, pages;
     int32_t prefix_len, prefix_splits, prefix_chunk, prefix_tiles, prefix_blocks;
     int32_t suffix_width, suffix_splits, suffix_chunk, suffix_tiles;
+    uint64_t page_bytes, page_rows;                   // of a page: all its heads
+    int32_t q_wide;                                   // queries can be read 16 bytes at a time
     float c;                                          // scale * log2(e): weights are powers of 2
 };
 
-enum : int { FEW = 0, MANY = 1 };                     // forms of a workgroup: 16 rows, its waves taking keys in turn; 128 rows, keys shared
-constexpr int kAttnThreads = 256;
-constexpr int kFewRows = 16, kManyRows = 128;
+// Forms of a workgroup: 16 rows whose waves take keys in turn; 64, or 128, rows that share their keys.
+enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2 };
+constexpr int kJoinThreads = 256;
+constexpr int kFormRows[] = {16, 64, 128};
 constexpr int kChunkStep = 128;                       // splits begin at multiples of this many keys: every tile is aligned
 constexpr int kMaxSplits = 256;                       // of a prefix, and of a suffix
 

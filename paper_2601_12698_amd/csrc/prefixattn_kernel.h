@@ -45,6 +45,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr float kLazy = 8.0f;                                   // a maximum may lag behind by this power of 2
 // fp16 weights are 2^7 times larger (at most 2^15), so that they are normal numbers down to 2^-21 of the largest.
 template <int DT> constexpr float kLift = DT == DT_FP16 ? 7.0f : 0.0f;
+constexpr uint64_t full_of(int bits) { return bits == 64 ? ~0ull : (1ull << bits) - 1; }
 constexpr float kNone = -__builtin_huge_valf();
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
@@ -68,9 +69,15 @@ __device__ __forceinline__ typename mat<DT>::T8 two_transposed(const char* lds_a
     return __builtin_bit_cast(typename mat<DT>::T8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-__device__ __forceinline__ float other_half_max(float x) { const pair p = with_half(x); return fmaxf(p.a, p.b); }
+// The larger of two, NaN if one is NaN: three operands an instruction, and unlike fmaxf without making signalling NaNs quiet first.
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+template <int ROWS> struct acc;
+template <> struct acc<16> { typedef f32x4 type; };
+template <> struct acc<32> { typedef f32x16 type; };
+
+__device__ __forceinline__ float other_half_max(float x) { const pair p = with_half(x); return larger(p.a, p.b); }
 __device__ __forceinline__ float other_half_sum(float x) { const pair p = with_half(x); return p.a + p.b; }
-__device__ __forceinline__ float other_row_max(float x) { const pair p = with_row(x); return fmaxf(p.a, p.b); }
+__device__ __forceinline__ float other_row_max(float x) { const pair p = with_row(x); return larger(p.a, p.b); }
 __device__ __forceinline__ float other_row_sum(float x) { const pair p = with_row(x); return p.a + p.b; }
 
 // A workgroup's share: rows [row0, row0 + rows) of a key head, rows counted token by token from token `token0`, keys
@@ -99,11 +106,30 @@ __device__ __forceinline__ Row row_of(const AttnArgs& a, const Share& s, int32_t
     return row;
 }
 
-// The cache row of a key: -1 where its page is outside the cache.
-__device__ __forceinline__ int64_t cache_row(const AttnArgs& a, int32_t head, int32_t page, int32_t key)
+// Where a key's elements and its scale lie.  Where its page is not in the cache, or the key is beyond the share's end, callers
+// take page 0 and set the piece to zeros afterwards: loads stand in no branch, so that all of a tile's are under way together.
+struct Place {
+    uint64_t bytes, row;
+};
+__device__ __forceinline__ Place place_of(const AttnArgs& a, int32_t head, int32_t page, int32_t key, int32_t row_bytes)
 {
-    const int64_t row = ((static_cast<int64_t>(page) * a.kv_heads + head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
-    return static_cast<uint32_t>(page) < static_cast<uint32_t>(a.pages) ? row : -1;
+    const uint32_t in = (static_cast<uint32_t>(head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));       // below 2^32 / row_bytes
+    return Place{static_cast<uint64_t>(page) * a.page_bytes + in * static_cast<uint32_t>(row_bytes), static_cast<uint64_t>(page) * a.page_rows + in};
+}
+__device__ __forceinline__ bool in_cache(const AttnArgs& a, int32_t page) { return static_cast<uint32_t>(page) < static_cast<uint32_t>(a.pages); }
+
+// Eight elements of a row's query from e on, zeros beyond the row or the head.
+template <int DT>
+__device__ __forceinline__ typename mat<DT>::T8 query_piece(const AttnArgs& a, const Row& row, int32_t e)
+{
+    typedef typename mat<DT>::T8 T8;
+    const auto* p = at_global<const typename mat<DT>::T>(a.q) + row.q + (e < a.d ? e : 0);
+    T8 x;
+    if (a.q_wide) x = *reinterpret_cast<const T8*>(p);
+    else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = p[j];
+    return row.in && e < a.d ? x : T8{};
 }
 
 template <int DT, int FORMAT, int DP>
@@ -113,6 +139,7 @@ struct Few {
     typedef typename M::T8 T8;
     static constexpr bool CODES = FORMAT == KVCACHE_E4M3;
     static constexpr int ES = CODES ? 1 : 2;
+    static constexpr int THREADS = 256, ROWS = 16;
     static constexpr int TILE = 32;                             // keys of a wave at a time
     static constexpr int NC = DP / 32;                          // steps of 32 elements in S
     static constexpr int NK = CODES ? NC / 2 : NC;              // 16-byte loads of a lane for 16 keys
@@ -122,20 +149,23 @@ struct Few {
     static constexpr int VROW = DP * 2 + 32;                    // bytes from key to key in LDS: 4 keys' 32 bytes fall on 4 groups of banks
     static constexpr int WAVE_LDS = TILE * VROW;
     static constexpr int OROW = DP + 4;                         // floats from row to row where waves are joined
-    static constexpr int LDS = 4 * WAVE_LDS > 4 * kFewRows * OROW * 4 ? 4 * WAVE_LDS : 4 * kFewRows * OROW * 4;
+    static constexpr int LDS = 4 * WAVE_LDS > 4 * ROWS * OROW * 4 ? 4 * WAVE_LDS : 4 * ROWS * OROW * 4;
 
     u32x4 k[2][NK], v[NV];
-    uint32_t scales;                                            // of key lane % 32: the key's byte, and the value's above it
+    uint32_t k_scale, v_scale;                                  // of key lane % 32
     uint32_t valid;                                             // keys of the tile that are there
 
+    // `page` is that of key lane % 32.
     __device__ __forceinline__ void load(const AttnArgs& a, const Share& s, int32_t key0, int32_t page, int lane)
     {
         const int32_t mine = key0 + (lane & 31);
-        const int64_t row = mine < s.end ? cache_row(a, s.head, page, mine) : -1;
-        valid = static_cast<uint32_t>(__ballot(row >= 0));
-        scales = 0;
+        const bool there = mine < s.end && in_cache(a, page);
+        valid = static_cast<uint32_t>(__ballot(there));
+        if (!there) page = 0;
         if constexpr (CODES) {
-            if (row >= 0) scales = at_global<const uint8_t>(a.k_scale)[row] | (at_global<const uint8_t>(a.v_scale)[row] << 8);
+            const uint64_t row = place_of(a, s.head, page, mine, 0).row;
+            k_scale = at_global<const uint8_t>(a.k_scale)[row];
+            v_scale = at_global<const uint8_t>(a.v_scale)[row];
         }
         const char* kp = at_global<const char>(a.k_pages);
         const char* vp = at_global<const char>(a.v_pages);
@@ -143,29 +173,39 @@ struct Few {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int at = 16 * t + (lane & 15);
-            const int64_t r = cache_row(a, s.head, __shfl(page, at), key0 + at);
-            const bool in = (valid >> at) & 1;
+            const char* r = kp + place_of(a, s.head, __shfl(page, at), key0 + at, row_bytes).bytes;
 #pragma unroll
             for (int c = 0; c < NK; ++c) {
                 const int32_t b = 64 * c + 16 * (lane >> 4);    // 16 bytes: 8 elements, or 16 codes
-                k[t][c] = u32x4{0, 0, 0, 0};
-                if (in && b < row_bytes) k[t][c] = *reinterpret_cast<const u32x4*>(kp + r * row_bytes + b);
+                k[t][c] = *reinterpret_cast<const u32x4*>(r + (b < row_bytes ? b : 0));
             }
         }
+        const int32_t b = 16 * (lane % PIECES);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = (64 / PIECES) * i + lane / PIECES;
-            const int32_t b = 16 * (lane % PIECES);
-            const int64_t r = cache_row(a, s.head, __shfl(page, at), key0 + at);
-            v[i] = u32x4{0, 0, 0, 0};
-            if (((valid >> at) & 1) && b < row_bytes) v[i] = *reinterpret_cast<const u32x4*>(vp + r * row_bytes + b);
+            v[i] = *reinterpret_cast<const u32x4*>(vp + place_of(a, s.head, __shfl(page, at), key0 + at, row_bytes).bytes + (b < row_bytes ? b : 0));
         }
+    }
+    // Zeros in the place of keys that are not there and of elements beyond the head.
+    __device__ __forceinline__ void clear(const AttnArgs& a, int lane)
+    {
+        const int32_t row_bytes = a.d * ES;
+        if (valid == 0xffffffffu && row_bytes == DP * ES) return;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < NK; ++c)
+                if (!((valid >> (16 * t + (lane & 15))) & 1) || 64 * c + 16 * (lane >> 4) >= row_bytes) k[t][c] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (!((valid >> ((64 / PIECES) * i + lane / PIECES)) & 1)) v[i] = u32x4{0, 0, 0, 0};
+        if (!((valid >> (lane & 31)) & 1)) k_scale = v_scale = 127;
     }
 
     static __device__ __forceinline__ int32_t page_of(const AttnArgs& a, const Share& s, int32_t key0, int lane)
     {
-        const int32_t key = key0 + (lane & 31);
-        return key < s.end ? s.table[key >> a.page_shift] : -1;
+        return s.table[min(key0 + (lane & 31), s.end - 1) >> a.page_shift];
     }
 
     __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, char* lds)
@@ -176,9 +216,7 @@ struct Few {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int32_t e = CODES ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
-            const T* p = at_global<const T>(a.q) + row.q + e;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[c][j] = row.in && e < a.d ? p[j] : static_cast<T>(0.0f);
+            q[c] = query_piece<DT>(a, row, e);
         }
         f32x4 o[NT];
 #pragma unroll
@@ -191,14 +229,15 @@ struct Few {
 
         int32_t key0 = s.first + TILE * wave;
         if (key0 < s.end) load(a, s, key0, page_of(a, s, key0, lane), lane);
-        int32_t page = key0 + 4 * TILE < s.end ? page_of(a, s, key0 + 4 * TILE, lane) : -1;
+        int32_t page = page_of(a, s, key0 + 4 * TILE, lane);
         while (key0 < s.end) {
+            clear(a, lane);
             // values to LDS, as elements
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int at = (64 / PIECES) * i + lane / PIECES, b = lane % PIECES;
                 if constexpr (CODES) {
-                    const float sc = scale_of((__shfl(scales, at) >> 8) & 255);
+                    const float sc = scale_of(__shfl(v_scale, at));
                     T8* to = reinterpret_cast<T8*>(mine + at * VROW + 32 * b);
                     to[0] = elements_of<DT>(v[i][0], v[i][1], sc);
                     to[1] = elements_of<DT>(v[i][2], v[i][3], sc);
@@ -212,7 +251,7 @@ struct Few {
             for (int t = 0; t < 2; ++t) {
                 z[t] = f32x4{0, 0, 0, 0};
                 if constexpr (CODES) {
-                    const float sc = scale_of(__shfl(scales, 16 * t + (lane & 15)) & 255);
+                    const float sc = scale_of(__shfl(k_scale, 16 * t + (lane & 15)));
 #pragma unroll
                     for (int c = 0; c < NK; ++c) {
                         z[t] = M::mul16(elements_of<DT>(k[t][c][0], k[t][c][1], sc), q[2 * c], z[t]);
@@ -228,21 +267,23 @@ struct Few {
             key0 += 4 * TILE;
             if (key0 < s.end) {
                 load(a, s, key0, page, lane);
-                page = key0 + 4 * TILE < s.end ? page_of(a, s, key0 + 4 * TILE, lane) : -1;
+                page = page_of(a, s, key0 + 4 * TILE, lane);
             }
             if (there != 0xffffffffu || now + TILE - 1 > s.last0) {
+                const uint32_t mine_there = there >> (4 * g);   // this lane's keys, shifted so that each is a fixed bit
+                const int32_t last = row.last - now - 4 * g;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int at = 16 * t + 4 * g + r;
-                        if (!((there >> at) & 1) || now + at > row.last) z[t][r] = kNone;
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        if (!((mine_there >> (16 * t + r)) & 1) || 16 * t + r > last) z[t][r] = kNone;
             }
-            float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+            float top = z[0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = larger(top, z[i >> 2][i & 3]);
             top = other_half_max(other_row_max(top));
             if (__any(top > m + lag)) {
-                const float next = fmaxf(m, top);
+                const float next = larger(m, top);
                 const float down = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - next) * a.c);
                 l *= down;
 #pragma unroll
@@ -270,12 +311,12 @@ struct Few {
 
         // the four waves' results, joined
         l = other_half_sum(other_row_sum(l));
-        __shared__ float2 ml[4][kFewRows];
+        __shared__ float2 ml[4][ROWS];
         if (lane < 16) ml[wave][lane] = make_float2(m, l);
         __syncthreads();
         float best = kNone, sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) best = fmaxf(best, ml[w][lane & 15].x);
+        for (int w = 0; w < 4; ++w) best = larger(best, ml[w][lane & 15].x);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float2 x = ml[w][lane & 15];
@@ -288,72 +329,86 @@ struct Few {
             f32x4 x = o[t];
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] *= down;
-            *reinterpret_cast<f32x4*>(join + (wave * kFewRows + (lane & 15)) * OROW + 16 * t + 4 * g) = x;
+            *reinterpret_cast<f32x4*>(join + (wave * ROWS + (lane & 15)) * OROW + 16 * t + 4 * g) = x;
         }
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
         if (wave == 0 && lane < 16 && row.in)
             at_global<float2>(a.part_ml)[s.part * rows + row.global] = make_float2(best == kNone ? kNone : best * a.c - kLift<DT>, sum);
         __syncthreads();
-        for (int i = threadIdx.x; i < kFewRows * DP / 4; i += kAttnThreads) {
+        for (int i = threadIdx.x; i < ROWS * DP / 4; i += THREADS) {
             const int r = i / (DP / 4), e = 4 * (i % (DP / 4));
             if (r >= s.rows || e >= a.d) continue;
             f32x4 x = *reinterpret_cast<const f32x4*>(join + r * OROW + e);
 #pragma unroll
-            for (int w = 1; w < 4; ++w) x += *reinterpret_cast<const f32x4*>(join + (w * kFewRows + r) * OROW + e);
+            for (int w = 1; w < 4; ++w) x += *reinterpret_cast<const f32x4*>(join + (w * ROWS + r) * OROW + e);
             *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + (s.part * rows + row_of(a, s, r).global) * a.d + e) = x;
         }
     }
 };
 
-template <int DT, int FORMAT, int DP>
+template <int DT, int FORMAT, int DP, int RW, int WAVES>
 struct Many {
     typedef mat<DT> M;
     typedef typename M::T T;
     typedef typename M::T8 T8;
-    static constexpr bool CODES = FORMAT == KVCACHE_E4M3;
-    static constexpr int ES = CODES ? 1 : 2;
-    static constexpr int TILE = 64;
-    static constexpr int NC = DP / 16;                          // steps of 16 elements in S
-    static constexpr int NT = DP / 32;                          // tiles of 32 elements in O
+    static constexpr bool CODES = FORMAT == KVCACHE_E4M3, WIDE = RW == 32;
+    static constexpr int ES = CODES ? 1 : 2, THREADS = 64 * WAVES, ROWS = RW * WAVES;
+    static constexpr int TILE = DP > 128 && WAVES == 4 ? 32 : 64;   // keys at a time: two workgroups' tiles, or one of eight waves, fit a CU
+    typedef typename acc<RW>::type A;                           // of a lane: WIDE 16 of 32 keys (or elements) by rows, else 4 of 16
+    static constexpr int AN = WIDE ? 16 : 4;
+    static constexpr int NS = TILE / RW;                        // pieces of S
+    static constexpr int KC = WIDE ? 16 : 32;                   // elements, or keys, that one matrix instruction sums over
+    static constexpr int NC = DP / KC;
+    static constexpr int NT = DP / RW;                          // pieces of O
     static constexpr int PIECES = DP * ES / 16;
-    static constexpr int NP = TILE * PIECES / kAttnThreads;     // pieces of keys, and of values, that a thread stages
-    static constexpr int KROW = DP * 2 + 16, VROW = DP * 2 + 32;   // bytes from key to key: 8 keys' 16, or 4 keys' 32, fall on all banks
+    static constexpr int NP = TILE * PIECES / THREADS;          // 16-byte pieces of keys, and of values, that a thread stages
+    static_assert(NP >= 1, "fewer pieces than threads");
+    // Bytes from key to key in LDS: lanes that are served together fall on different banks, 8 or 16 keys' 16 bytes for the keys,
+    // and for a transposing read of the values 4 keys' 64 bytes (WIDE) or 8 keys' 32.
+    static constexpr int KROW = DP * 2 + 16, VROW = DP * 2 + (WIDE ? 64 : 32);
     static constexpr int BUF = TILE * (KROW + VROW) + TILE;     // keys, values, a byte for each key that is there
     static constexpr int LDS = 2 * BUF;
 
     u32x4 k[NP], v[NP];
-    uint32_t scales[NP];                                        // the key's byte, the value's above it, and 2^16 if the key is there
+    uint32_t k_scale[NP], v_scale[NP];
+    uint32_t valid;                                             // bit i: the key of piece i is there
 
-    static __device__ __forceinline__ int key_of(int i) { return (kAttnThreads / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
+    static __device__ __forceinline__ int key_of(int i) { return (THREADS / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
     static __device__ __forceinline__ int piece() { return static_cast<int>(threadIdx.x) % PIECES; }
 
-    __device__ __forceinline__ void pages_of(const AttnArgs& a, const Share& s, int32_t key0, int32_t (&page)[NP]) const
+    static __device__ __forceinline__ void pages_of(const AttnArgs& a, const Share& s, int32_t key0, int32_t (&page)[NP])
     {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int32_t key = key0 + key_of(i);
-            page[i] = key < s.end ? s.table[key >> a.page_shift] : -1;
-        }
+        for (int i = 0; i < NP; ++i) page[i] = s.table[min(key0 + key_of(i), s.end - 1) >> a.page_shift];
     }
     __device__ __forceinline__ void load(const AttnArgs& a, const Share& s, int32_t key0, const int32_t (&page)[NP])
     {
-        const char* kp = at_global<const char>(a.k_pages);
-        const char* vp = at_global<const char>(a.v_pages);
-        const int32_t row_bytes = a.d * ES, b = 16 * piece();
+        const int32_t row_bytes = a.d * ES, b = 16 * piece() < row_bytes ? 16 * piece() : 0;
+        valid = 0;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int64_t row = cache_row(a, s.head, page[i], key0 + key_of(i));
-            k[i] = v[i] = u32x4{0, 0, 0, 0};
-            scales[i] = 0;
-            if (row >= 0) {
-                if (b < row_bytes) {
-                    k[i] = *reinterpret_cast<const u32x4*>(kp + row * row_bytes + b);
-                    v[i] = *reinterpret_cast<const u32x4*>(vp + row * row_bytes + b);
-                }
-                scales[i] = 1u << 16;
-                if constexpr (CODES) scales[i] |= at_global<const uint8_t>(a.k_scale)[row] | (at_global<const uint8_t>(a.v_scale)[row] << 8);
+            const bool there = key0 + key_of(i) < s.end && in_cache(a, page[i]);
+            valid |= there ? 1u << i : 0u;
+            const Place p = place_of(a, s.head, there ? page[i] : 0, key0 + key_of(i), row_bytes);
+            k[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.k_pages) + (p.bytes + b));
+            v[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.v_pages) + (p.bytes + b));
+            if constexpr (CODES) {
+                k_scale[i] = at_global<const uint8_t>(a.k_scale)[p.row];
+                v_scale[i] = at_global<const uint8_t>(a.v_scale)[p.row];
             }
         }
+    }
+    // Zeros in the place of keys that are not there and of elements beyond the head.
+    __device__ __forceinline__ void clear(const AttnArgs& a)
+    {
+        const bool in = 16 * piece() < a.d * ES;
+        if (__all(in && valid == (1u << NP) - 1)) return;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            if (!in || !((valid >> i) & 1)) {
+                k[i] = v[i] = u32x4{0, 0, 0, 0};
+                k_scale[i] = v_scale[i] = 127;
+            }
     }
     __device__ __forceinline__ void stage(char* buf) const
     {
@@ -362,7 +417,7 @@ struct Many {
             char* kt = buf + key_of(i) * KROW + (CODES ? 32 : 16) * piece();
             char* vt = buf + TILE * KROW + key_of(i) * VROW + (CODES ? 32 : 16) * piece();
             if constexpr (CODES) {
-                const float ks = scale_of(scales[i] & 255), vs = scale_of((scales[i] >> 8) & 255);
+                const float ks = scale_of(k_scale[i]), vs = scale_of(v_scale[i]);
                 reinterpret_cast<T8*>(kt)[0] = elements_of<DT>(k[i][0], k[i][1], ks);
                 reinterpret_cast<T8*>(kt)[1] = elements_of<DT>(k[i][2], k[i][3], ks);
                 reinterpret_cast<T8*>(vt)[0] = elements_of<DT>(v[i][0], v[i][1], vs);
@@ -371,34 +426,37 @@ struct Many {
                 *reinterpret_cast<u32x4*>(kt) = k[i];
                 *reinterpret_cast<u32x4*>(vt) = v[i];
             }
-            if (piece() == 0) buf[TILE * (KROW + VROW) + key_of(i)] = static_cast<char>(scales[i] >> 16);
+            if (piece() == 0) buf[TILE * (KROW + VROW) + key_of(i)] = static_cast<char>((valid >> i) & 1);
         }
+    }
+
+    static __device__ __forceinline__ A mul(T8 a, T8 b, A c)
+    {
+        if constexpr (WIDE) return M::template mul32<A>(a, b, c);
+        else return M::mul16(a, b, c);
     }
 
     __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, char* lds)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-        const Row row = row_of(a, s, 32 * wave + (lane & 31));
-        const bool busy = 32 * wave < s.rows;                   // waves without rows only help to stage
-        T8 q[NC];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int32_t e = 16 * c + 8 * h;
-            const T* p = at_global<const T>(a.q) + row.q + e;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[c][j] = row.in && e < a.d ? p[j] : static_cast<T>(0.0f);
-        }
-        f32x16 o[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) o[t] = f32x16{};
-        float m = kNone, l = 0.0f;
-        const float lag = kLazy / a.c;
-
+        // lane = row, and one of 2 (WIDE) or 4 groups of keys or elements
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
         int32_t page[NP];
         int32_t key0 = s.first;
         pages_of(a, s, key0, page);
+        const Row row = row_of(a, s, RW * wave + r);
+        const bool busy = RW * wave < s.rows;                   // waves without rows only help to stage
         load(a, s, key0, page);
+        T8 q[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) q[c] = query_piece<DT>(a, row, KC * c + 8 * g);
+        A o[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[t] = A{};
+        float m = kNone, l = 0.0f;
+        const float lag = kLazy / a.c;
+
         pages_of(a, s, key0 + TILE, page);
+        clear(a);
         stage(lds);
         __syncthreads();
         for (int cur = 0; key0 < s.end; key0 += TILE, cur ^= 1) {
@@ -409,70 +467,79 @@ struct Many {
             }
             const char* buf = lds + cur * BUF;
             if (busy) {
-                const char* kt = buf + (lane & 31) * KROW + 16 * h;
-                f32x16 z[2];
+                const char* kt = buf + r * KROW + 16 * g;
+                A z[NS];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    z[t] = f32x16{};
+                for (int t = 0; t < NS; ++t) {
+                    z[t] = A{};
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) z[t] = M::mul32(*reinterpret_cast<const T8*>(kt + 32 * t * KROW + 32 * c), q[c], z[t]);
+                    for (int c = 0; c < NC; ++c) z[t] = mul(*reinterpret_cast<const T8*>(kt + RW * t * KROW + 2 * KC * c), q[c], z[t]);
                 }
-                const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane] != 0);
-                if (there != ~0ull || key0 + TILE - 1 > s.last0) {
+                const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane % TILE] != 0) & full_of(TILE);
+                if (there != full_of(TILE) || key0 + TILE - 1 > s.last0) {
+                    // this lane's keys, shifted so that each is a fixed bit (a mask made for every score would be held in registers)
+                    const uint64_t mine = there >> (4 * g);
+                    const int32_t last = row.last - key0 - 4 * g;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
+                    for (int t = 0; t < NS; ++t)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int at = 32 * t + 8 * (i >> 2) + 4 * h + (i & 3);
-                            if (!((there >> at) & 1) || key0 + at > row.last) z[t][i] = kNone;
+                        for (int i = 0; i < AN; ++i) {
+                            const int at = RW * t + (WIDE ? 8 * (i >> 2) : 0) + (i & 3);
+                            if (!((mine >> at) & 1) || at > last) z[t][i] = kNone;
                         }
                 }
                 float top = z[0][0];
 #pragma unroll
-                for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i >> 4][i & 15]);
+                for (int i = 1; i < NS * AN; ++i) top = larger(top, z[i / AN][i % AN]);
+                if constexpr (!WIDE) top = other_row_max(top);
                 top = other_half_max(top);
                 if (__any(top > m + lag)) {
-                    const float next = fmaxf(m, top);
+                    const float next = larger(m, top);
                     const float down = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - next) * a.c);
                     l *= down;
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[t][i] *= down;
+                        for (int i = 0; i < AN; ++i) o[t][i] *= down;
                     m = next;
                 }
                 const float base = m == kNone ? 0.0f : m * a.c - kLift<DT>;
-                // where this lane's 8 bytes of a transposing read begin: key 4 h + (lane % 16) / 4, elements 16 ((lane / 16) % 2) + 4 (lane % 4)
-                const char* vt = buf + TILE * KROW + (4 * h + ((lane & 15) >> 2)) * VROW + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+                // where this lane's 8 bytes of a transposing read begin: of 4 keys, its (lane % 16) / 4 th, elements 4 (lane % 4) of 16
+                const char* vt = buf + TILE * KROW + (4 * g + ((lane & 15) >> 2)) * VROW + (WIDE ? 32 * ((lane >> 4) & 1) : 0) + 8 * (lane & 3);
 #pragma unroll
-                for (int u = 0; u < TILE / 16; ++u) {
+                for (int u = 0; u < TILE / KC; ++u) {
                     T8 p;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u >> 1][8 * (u & 1) + j], a.c, -base));
+                        const float x = WIDE ? z[u / 2][(8 * u + j) % AN] : z[2 * u + j / 4][j % 4];
+                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.c, -base));
                         l += w;
                         p[j] = static_cast<T>(w);
                     }
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const char* at = vt + 16 * u * VROW + 64 * t;
-                        o[t] = M::mul32(two_transposed<DT>(at, at + 8 * VROW), p, o[t]);
+                        const char* at = vt + KC * u * VROW + 2 * RW * t;
+                        o[t] = mul(two_transposed<DT>(at, at + KC / 2 * VROW), p, o[t]);
                     }
                 }
             }
-            if (more) stage(lds + (cur ^ 1) * BUF);
+            if (more) {
+                clear(a);
+                stage(lds + (cur ^ 1) * BUF);
+            }
             __syncthreads();
         }
         if (!busy) return;
+        if constexpr (!WIDE) l = other_row_sum(l);
         l = other_half_sum(l);
         if (!row.in) return;
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads, at = s.part * rows + row.global;
-        if (h == 0) at_global<float2>(a.part_ml)[at] = make_float2(m == kNone ? kNone : m * a.c - kLift<DT>, l);
+        if (g == 0) at_global<float2>(a.part_ml)[at] = make_float2(m == kNone ? kNone : m * a.c - kLift<DT>, l);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t e = 32 * t + 8 * i + 4 * h;
+            for (int i = 0; i < AN / 4; ++i) {
+                const int32_t e = RW * t + 8 * i + 4 * g;
                 if (e < a.d)
                     *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + at * a.d + e) = f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
             }
@@ -481,53 +548,55 @@ struct Many {
 
 // Workgroups of the prefix first, then those of the suffixes.  Workgroups go round the 8 XCDs; the row tiles of one head and
 // key range stand 8 apart, so that they read it through the same L2 at the same time.
+// FORM: see prefixattn_args.h.
+template <int DT, int FORMAT, int DP, int FORM> struct form;
+template <int DT, int FORMAT, int DP> struct form<DT, FORMAT, DP, FEW> { typedef Few<DT, FORMAT, DP> type; };
+template <int DT, int FORMAT, int DP> struct form<DT, FORMAT, DP, MANY_64> { typedef Many<DT, FORMAT, DP, 16, 4> type; };
+template <int DT, int FORMAT, int DP> struct form<DT, FORMAT, DP, MANY_128> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4)> type; };
+
 template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX>
-__global__ __launch_bounds__(kAttnThreads, DP > 128 ? 1 : 2) void attn_kernel(const AttnArgs a)
+__global__ __launch_bounds__((form<DT, FORMAT, DP, PREFIX>::type::THREADS), 2) void attn_kernel(const AttnArgs a)
 {
-    typedef Few<DT, FORMAT, DP> F;
-    typedef Many<DT, FORMAT, DP> N;
-    constexpr int LDS = PREFIX == MANY || SUFFIX == MANY ? (N::LDS > F::LDS || SUFFIX == MANY ? N::LDS : F::LDS) : F::LDS;
-    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    typedef typename form<DT, FORMAT, DP, PREFIX>::type P;
+    typedef typename form<DT, FORMAT, DP, SUFFIX>::type S;
+    __shared__ __attribute__((aligned(16))) char lds[P::LDS > S::LDS ? P::LDS : S::LDS];
     int32_t b = static_cast<int32_t>(blockIdx.x);
     Share s;
     if (b < a.prefix_blocks) {
         const int32_t j = b >> 3, tile = j % a.prefix_tiles, pair = (j / a.prefix_tiles) * 8 + (b & 7);
         if (pair >= a.prefix_splits * a.kv_heads) return;
         const int32_t split = pair / a.kv_heads;
-        constexpr int ROWS = PREFIX == MANY ? kManyRows : kFewRows;
         s.head = pair - split * a.kv_heads;
         s.table = at_global<const int32_t>(a.prefix_pages);
         s.token0 = 0;
-        s.row0 = tile * ROWS;
-        s.rows = min(ROWS, a.batch * a.q_len * a.group - s.row0);
+        s.row0 = tile * P::ROWS;
+        s.rows = min(P::ROWS, a.batch * a.q_len * a.group - s.row0);
         s.first = split * a.prefix_chunk;
         s.end = min(s.first + a.prefix_chunk, a.prefix_len);
         s.part = split;
         s.last0 = kAll;
-        if constexpr (PREFIX == MANY) N().run(a, s, lds);
-        else F().run(a, s, lds);
+        P().run(a, s, lds);
         return;
     }
+    if (threadIdx.x >= S::THREADS) return;                      // a form with more waves than the suffixes' leaves the others idle
     b -= a.prefix_blocks;
     const int32_t seq = b / (a.suffix_tiles * a.suffix_splits * a.kv_heads);
     b -= seq * a.suffix_tiles * a.suffix_splits * a.kv_heads;
     const int32_t split = b / (a.suffix_tiles * a.kv_heads);
     b -= split * a.suffix_tiles * a.kv_heads;
     const int32_t tile = b / a.kv_heads;
-    constexpr int ROWS = SUFFIX == MANY ? kManyRows : kFewRows;
     const int32_t keys = min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), a.suffix_width << a.page_shift);
     s.head = b - tile * a.kv_heads;
     s.table = at_global<const int32_t>(a.suffix_pages) + static_cast<int64_t>(seq) * a.suffix_width;
     s.token0 = seq * a.q_len;
-    s.row0 = tile * ROWS;
-    s.rows = min(ROWS, a.q_len * a.group - s.row0);
+    s.row0 = tile * S::ROWS;
+    s.rows = min(S::ROWS, a.q_len * a.group - s.row0);
     s.first = split * a.suffix_chunk;
     s.end = min(s.first + a.suffix_chunk, keys);
     s.part = a.prefix_splits + split;
     s.last0 = keys - a.q_len;
     if (s.first >= s.end) return;                               // the joining kernel knows the length, too
-    if constexpr (SUFFIX == MANY) N().run(a, s, lds);
-    else F().run(a, s, lds);
+    S().run(a, s, lds);
 }
 
 }  // namespace serving

@@ -2,12 +2,24 @@
 #include "prefixattn_kernel.h"
 
 namespace serving {
+namespace {
 
+template <int PREFIX, int SUFFIX>
+void launch(const AttnArgs& a, unsigned blocks, hipStream_t s)
+{
+    attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX, SUFFIX><<<blocks, form<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX>::type::THREADS, 0, s>>>(a);
+}
+
+}  // namespace
+
+// A sequence's rows are some of the prefix's rows, so that its form is never the larger one.
 hipError_t ATTN_UNIT(UNIT_DT, UNIT_FORMAT, UNIT_DP)(const AttnArgs& a, int prefix_form, int suffix_form, unsigned blocks, hipStream_t s)
 {
-    if (prefix_form == FEW) attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, FEW, FEW><<<blocks, kAttnThreads, 0, s>>>(a);
-    else if (suffix_form == FEW) attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, MANY, FEW><<<blocks, kAttnThreads, 0, s>>>(a);
-    else attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, MANY, MANY><<<blocks, kAttnThreads, 0, s>>>(a);
+    if (prefix_form == FEW) launch<FEW, FEW>(a, blocks, s);
+    else if (prefix_form == MANY_64) suffix_form == FEW ? launch<MANY_64, FEW>(a, blocks, s) : launch<MANY_64, MANY_64>(a, blocks, s);
+    else if (suffix_form == FEW) launch<MANY_128, FEW>(a, blocks, s);
+    else if (suffix_form == MANY_64) launch<MANY_128, MANY_64>(a, blocks, s);
+    else launch<MANY_128, MANY_128>(a, blocks, s);
     return hipGetLastError();
 }
 
