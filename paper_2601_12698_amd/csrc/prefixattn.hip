@@ -12,50 +12,81 @@ using namespace serving;
 namespace {
 
 // out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, lse = ln 2 (m + log2 of that sum), over the parts that were run: a suffix
-// has as many as its length says.  A workgroup joins one row; its threads are columns of four elements by groups of parts.
-template <int DT>
+// has as many as its length says.  WAVES waves join a row, lanes being columns of four elements by groups of parts; the first parts
+// are under way while their weights are found.  One wave where there are rows enough to fill the chip (no barrier, four rows a
+// workgroup), four where there are few rows, which then have many parts.
+template <int DT, int WAVES>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttnArgs a)
 {
     typedef typename elem<DT>::type T;
     typedef T T4 __attribute__((ext_vector_type(4)));
-    __shared__ float weight[2 * kMaxSplits], red[2][4];
+    constexpr int ROWS = kJoinThreads / 64 / WAVES, THREADS = 64 * WAVES, AHEAD = 4;
+    __shared__ float weight[ROWS][2 * kMaxSplits], red[2][4];
     __shared__ f32x4 sums[kJoinThreads];
-    const int32_t row = static_cast<int32_t>(blockIdx.x), tid = static_cast<int32_t>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+    const int32_t tid = static_cast<int32_t>(threadIdx.x) % THREADS, slot = static_cast<int32_t>(threadIdx.x) / THREADS, wave = tid >> 6;
     const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
+    const int32_t row = static_cast<int32_t>(blockIdx.x) * ROWS + slot;
+    if (row >= rows) return;                                    // with one wave a row: no barrier follows
+    const auto meet = [] {
+        if constexpr (WAVES > 1) __syncthreads();
+        else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
     int32_t parts = a.prefix_splits;
     if (a.suffix_splits) {
         const int32_t keys = min(max(at_global<const int32_t>(a.suffix_lens)[row / (a.q_len * a.q_heads)], 0), a.suffix_width << a.page_shift);
         parts += (keys + a.suffix_chunk - 1) / a.suffix_chunk;
     }
+    const int32_t cols = a.d / 4, groups = THREADS / cols, grp = tid / cols, col = tid - grp * cols;
+    const int64_t step = static_cast<int64_t>(groups) * rows * a.d;
+    const float* o = at_global<const float>(a.part_o) + (grp * rows + row) * a.d + 4 * col;
+    const int32_t mine = grp < groups && grp < parts ? (parts - grp + groups - 1) / groups : 0;      // parts that this lane adds
+    f32x4 first[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) first[i] = i < mine ? *reinterpret_cast<const f32x4*>(o + i * step) : f32x4{0, 0, 0, 0};
     const float2* ml = at_global<const float2>(a.part_ml);
     float m = -__builtin_huge_valf();
-    for (int32_t p = tid; p < parts; p += kJoinThreads) m = fmaxf(m, ml[p * rows + row].x);
+    for (int32_t p = tid; p < parts; p += THREADS) m = fmaxf(m, ml[p * rows + row].x);
 #pragma unroll
     for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-    if (lane == 0) red[0][wave] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    if constexpr (WAVES > 1) {
+        if ((tid & 63) == 0) red[0][wave] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    }
     float l = 0.0f;
-    for (int32_t p = tid; p < parts; p += kJoinThreads) {
+    for (int32_t p = tid; p < parts; p += THREADS) {
         const float2 x = ml[p * rows + row];
         // a part that saw no key has m = -inf, l = 0 and O = 0 (l is NaN where its scores were)
         const float w = x.x == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f(x.x - m);
-        weight[p] = w;
+        weight[slot][p] = w;
         l += w * x.y;
     }
 #pragma unroll
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
-    if (lane == 0) red[1][wave] = l;
-    __syncthreads();
-    l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-    const int32_t cols = a.d / 4, groups = kJoinThreads / cols, grp = tid / cols, col = tid - grp * cols;
+    if constexpr (WAVES > 1) {
+        if ((tid & 63) == 0) red[1][wave] = l;
+    }
+    meet();
+    if constexpr (WAVES > 1) l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
     f32x4 x = {0, 0, 0, 0};
-    if (grp < groups)
-        for (int32_t p = grp; p < parts; p += groups) x += weight[p] * *reinterpret_cast<const f32x4*>(at_global<const float>(a.part_o) + (p * rows + row) * a.d + 4 * col);
-    sums[tid] = x;
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < mine) x += weight[slot][grp + i * groups] * first[i];
+    for (int32_t i = AHEAD; i < mine; i += AHEAD) {
+        f32x4 next[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) next[j] = *reinterpret_cast<const f32x4*>(o + min(i + j, mine - 1) * step);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (i + j < mine) x += weight[slot][grp + (i + j) * groups] * next[j];
+    }
+    sums[threadIdx.x] = x;
+    meet();
     if (grp == 0) {
-        for (int32_t g = 1; g < groups; ++g) x += sums[g * cols + col];
+        for (int32_t g = 1; g < groups; ++g) x += sums[slot * THREADS + g * cols + col];
         const float inverse = l == 0.0f ? 0.0f : 1.0f / l;              // no key was seen: zeros
         T4 y;
 #pragma unroll
@@ -67,6 +98,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttnArgs a)
 
 constexpr int64_t kMaxBlocks = 1 << 24;      // of 256 threads: a launch has fewer than 2^32
 constexpr int32_t kMinChunk = 256;
+constexpr int64_t kFinishUnits = 256;        // from here on the suffixes alone fill the chip
+constexpr int64_t kJoinRows = 1024;          // from here on a wave joins a row: 4 waves a CU
 
 int32_t splits_of(int64_t keys, int64_t units, int64_t wanted, int32_t* chunk)
 {
@@ -82,7 +115,8 @@ int32_t splits_of(int64_t keys, int64_t units, int64_t wanted, int32_t* chunk)
 struct Plan {
     AttnArgs a;
     int prefix_form, suffix_form, dp;
-    int64_t rows, blocks, bytes;
+    int64_t rows, prefix_blocks, suffix_blocks, bytes;
+    bool finish;                             // the suffixes' workgroups are a launch of their own that joins the prefix's parts
 };
 
 // Checks a shape and splits its work.  A key range is split until there are two workgroups a CU (three of the form for few rows),
@@ -118,28 +152,31 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld queries of %d heads are beyond the limit (2^24 together)", (long long)tokens, s->q_heads);
     p->rows = tokens * s->q_heads;
     const int64_t all = tokens * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
-    auto form_of = [](int64_t rows) { return rows <= 16 ? FEW : rows <= 64 ? MANY_64 : MANY_128; };
+    auto form_of = [p](int64_t rows) { return rows <= 16 ? FEW : rows <= 64 ? MANY_64 : rows <= 128 || p->dp != 128 ? MANY_128 : MANY_256; };
     auto tiles = [](int64_t rows, int form) { return (rows + kFormRows[form] - 1) / kFormRows[form]; };
     p->suffix_form = form_of(own);
     p->prefix_form = form_of(all);
     // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
+    // a CU holds one workgroup of eight waves, two of four that share keys, three of those with few rows
+    auto wanted = [p](int form) { return form == FEW ? 768 : form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
     if (a.prefix_len && a.pages) {
         a.prefix_tiles = static_cast<int32_t>(tiles(all, p->prefix_form));
-        a.prefix_splits = splits_of(a.prefix_len, static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, p->prefix_form == FEW ? 768 : 512, &a.prefix_chunk);
-        p->blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
+        a.prefix_splits = splits_of(a.prefix_len, static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, wanted(p->prefix_form), &a.prefix_chunk);
+        p->prefix_blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
     } else {
         p->prefix_form = p->suffix_form;
     }
-    const int64_t prefix_blocks = p->blocks;
+    int64_t parts = a.prefix_splits;
     if (width && a.pages) {
         a.suffix_tiles = static_cast<int32_t>(tiles(own, p->suffix_form));
         const int64_t units = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads * s->batch;
-        a.suffix_splits = splits_of(width, units, p->suffix_form == FEW ? 768 : 512, &a.suffix_chunk);
-        p->blocks += units * a.suffix_splits;
+        p->finish = units >= kFinishUnits && a.prefix_splits <= kFinishSplits;
+        a.suffix_splits = splits_of(width, units, p->finish ? 1 : wanted(p->suffix_form), &a.suffix_chunk);
+        p->suffix_blocks = units * a.suffix_splits;
+        if (!p->finish) parts += a.suffix_splits;
     }
-    if (p->blocks > kMaxBlocks) return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)p->blocks);
-    a.prefix_blocks = static_cast<int32_t>(prefix_blocks);
-    const int64_t parts = a.prefix_splits + a.suffix_splits;
+    if (p->prefix_blocks + p->suffix_blocks > kMaxBlocks)
+        return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)(p->prefix_blocks + p->suffix_blocks));
     p->bytes = parts * p->rows * (4ll * a.d + 8);
     return ADDRMS_OK;
 }
@@ -174,7 +211,7 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
     if (shape->batch == 0 || shape->q_len == 0) return ADDRMS_OK;
     AttnArgs& a = p.a;
     const bool codes = shape->format == KVCACHE_E4M3, keys = a.prefix_splits || a.suffix_splits;
-    if (!q || !q_strides || !out || (keys && (!k_pages || !v_pages || !workspace || (codes && (!k_scale || !v_scale)))) ||
+    if (!q || !q_strides || !out || (keys && (!k_pages || !v_pages || (p.bytes && !workspace) || (codes && (!k_scale || !v_scale)))) ||
         (a.prefix_splits && !prefix_pages) || (a.suffix_splits && (!suffix_pages || !suffix_lens)))
         return fail(ADDRMS_ERR_INVALID_ARG, "no pointer may be NULL");
     if (workspace_bytes < p.bytes)
@@ -185,20 +222,28 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
     a.q = addr(q), a.k_pages = addr(k_pages), a.v_pages = addr(v_pages), a.k_scale = addr(k_scale), a.v_scale = addr(v_scale);
     a.prefix_pages = addr(prefix_pages), a.suffix_pages = addr(suffix_pages), a.suffix_lens = addr(suffix_lens), a.out = addr(out), a.lse = addr(lse);
     a.part_o = addr(workspace);
-    a.part_ml = a.part_o + 4ull * (a.prefix_splits + a.suffix_splits) * p.rows * a.d;
+    a.part_ml = a.part_o + 4ull * (p.bytes / (4ll * a.d + 8)) * a.d;
     a.q_token = q_strides[0], a.q_head = q_strides[1];
     a.q_wide = (a.q | static_cast<uint64_t>(q_strides[0] * 2) | static_cast<uint64_t>(q_strides[1] * 2)) % 16 == 0;
     a.c = scale * 1.44269504088896340736f;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (p.blocks) {
-        static constexpr AttnLaunch kUnits[2][2][3] = {
-            {{ATTN_UNIT(0, 0, 64), ATTN_UNIT(0, 0, 128), ATTN_UNIT(0, 0, 256)}, {ATTN_UNIT(0, 1, 64), ATTN_UNIT(0, 1, 128), ATTN_UNIT(0, 1, 256)}},
-            {{ATTN_UNIT(1, 0, 64), ATTN_UNIT(1, 0, 128), ATTN_UNIT(1, 0, 256)}, {ATTN_UNIT(1, 1, 64), ATTN_UNIT(1, 1, 128), ATTN_UNIT(1, 1, 256)}}};
-        const AttnLaunch unit = kUnits[shape->dtype == ADDRMS_FP16][codes][p.dp == 64 ? 0 : p.dp == 128 ? 1 : 2];
-        SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.blocks), s));
+    static constexpr AttnLaunch kUnits[2][2][3] = {
+        {{ATTN_UNIT(0, 0, 64), ATTN_UNIT(0, 0, 128), ATTN_UNIT(0, 0, 256)}, {ATTN_UNIT(0, 1, 64), ATTN_UNIT(0, 1, 128), ATTN_UNIT(0, 1, 256)}},
+        {{ATTN_UNIT(1, 0, 64), ATTN_UNIT(1, 0, 128), ATTN_UNIT(1, 0, 256)}, {ATTN_UNIT(1, 1, 64), ATTN_UNIT(1, 1, 128), ATTN_UNIT(1, 1, 256)}}};
+    const AttnLaunch unit = kUnits[shape->dtype == ADDRMS_FP16][codes][p.dp == 64 ? 0 : p.dp == 128 ? 1 : 2];
+    a.prefix_blocks = static_cast<int32_t>(p.prefix_blocks);
+    if (p.finish) {
+        if (p.prefix_blocks) SERVING_HIP_TRY(unit(a, p.prefix_form, p.prefix_form == FEW ? FEW : p.suffix_form, static_cast<unsigned>(p.prefix_blocks), s));
+        a.finish = 1;
+        a.prefix_blocks = 0;
+        SERVING_HIP_TRY(unit(a, p.suffix_form, p.suffix_form, static_cast<unsigned>(p.suffix_blocks), s));
+        return ADDRMS_OK;
     }
-    if (shape->dtype == ADDRMS_FP16) join_kernel<DT_FP16><<<static_cast<unsigned>(p.rows), kJoinThreads, 0, s>>>(a);
-    else join_kernel<DT_BF16><<<static_cast<unsigned>(p.rows), kJoinThreads, 0, s>>>(a);
+    if (p.prefix_blocks + p.suffix_blocks) SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.prefix_blocks + p.suffix_blocks), s));
+    const bool many = p.rows >= kJoinRows;
+    const unsigned groups = static_cast<unsigned>(many ? (p.rows + 3) / 4 : p.rows);
+    if (shape->dtype == ADDRMS_FP16) many ? join_kernel<DT_FP16, 1><<<groups, kJoinThreads, 0, s>>>(a) : join_kernel<DT_FP16, 4><<<groups, kJoinThreads, 0, s>>>(a);
+    else many ? join_kernel<DT_BF16, 1><<<groups, kJoinThreads, 0, s>>>(a) : join_kernel<DT_BF16, 4><<<groups, kJoinThreads, 0, s>>>(a);
     SERVING_HIP_TRY(hipGetLastError());
     return ADDRMS_OK;
 }

@@ -14,15 +14,17 @@ struct AttnArgs {
     int32_t prefix_len, prefix_splits, prefix_chunk, prefix_tiles, prefix_blocks;
     int32_t suffix_width, suffix_splits, suffix_chunk, suffix_tiles;
     uint64_t page_bytes, page_rows;                   // of a page: all its heads
+    int32_t finish;                                   // the suffixes' workgroups join the prefix's parts to their own, and write the output
     int32_t q_wide;                                   // queries can be read 16 bytes at a time
     float c;                                          // scale * log2(e): weights are powers of 2
 };
 
-// Forms of a workgroup: 16 rows whose waves take keys in turn; 64, or 128, rows that share their keys.
-enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2 };
+// Forms of a workgroup: 16 rows whose waves take keys in turn; 64, 128 or 256 rows that share their keys (256: heads of 65 to 128).
+enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2, MANY_256 = 3 };
 constexpr int kJoinThreads = 256;
-constexpr int kFormRows[] = {16, 64, 128};
+constexpr int kFormRows[] = {16, 64, 128, 256};
 constexpr int kChunkStep = 128;                       // splits begin at multiples of this many keys: every tile is aligned
+constexpr int kFinishSplits = 64;                     // of a prefix that is joined by the suffixes' workgroups: a part a lane
 constexpr int kMaxSplits = 256;                       // of a prefix, and of a suffix
 
 // One for each element type, format and padded head size (prefixattn_unit.hip).

@@ -71,6 +71,9 @@ __device__ __forceinline__ typename mat<DT>::T8 two_transposed(const char* lds_a
 
 // The larger of two, NaN if one is NaN: three operands an instruction, and unlike fmaxf without making signalling NaNs quiet first.
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+// ln 2 (m + log2 l): -infinity where no key was seen.
+__device__ __forceinline__ float lse_of(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f; }
+
 template <int ROWS> struct acc;
 template <> struct acc<16> { typedef f32x4 type; };
 template <> struct acc<32> { typedef f32x16 type; };
@@ -132,14 +135,14 @@ __device__ __forceinline__ typename mat<DT>::T8 query_piece(const AttnArgs& a, c
     return row.in && e < a.d ? x : T8{};
 }
 
-template <int DT, int FORMAT, int DP>
+template <int DT, int FORMAT, int DP, int WAVES>
 struct Few {
     typedef mat<DT> M;
     typedef typename M::T T;
     typedef typename M::T8 T8;
     static constexpr bool CODES = FORMAT == KVCACHE_E4M3;
     static constexpr int ES = CODES ? 1 : 2;
-    static constexpr int THREADS = 256, ROWS = 16;
+    static constexpr int THREADS = 64 * WAVES, ROWS = 16;
     static constexpr int TILE = 32;                             // keys of a wave at a time
     static constexpr int NC = DP / 32;                          // steps of 32 elements in S
     static constexpr int NK = CODES ? NC / 2 : NC;              // 16-byte loads of a lane for 16 keys
@@ -149,7 +152,7 @@ struct Few {
     static constexpr int VROW = DP * 2 + 32;                    // bytes from key to key in LDS: 4 keys' 32 bytes fall on 4 groups of banks
     static constexpr int WAVE_LDS = TILE * VROW;
     static constexpr int OROW = DP + 4;                         // floats from row to row where waves are joined
-    static constexpr int LDS = 4 * WAVE_LDS > 4 * ROWS * OROW * 4 ? 4 * WAVE_LDS : 4 * ROWS * OROW * 4;
+    static constexpr int LDS = WAVES * (WAVE_LDS > ROWS * OROW * 4 ? WAVE_LDS : ROWS * OROW * 4);
 
     u32x4 k[2][NK], v[NV];
     uint32_t k_scale, v_scale;                                  // of key lane % 32
@@ -227,9 +230,11 @@ struct Few {
         // where this lane's 8 bytes of a transposing read begin: key 4 g + (lane % 16) / 4 of 16, elements 4 (lane % 4) of 16
         const char* from = mine + (4 * g + ((lane & 15) >> 2)) * VROW + 8 * (lane & 3);
 
-        int32_t key0 = s.first + TILE * wave;
-        if (key0 < s.end) load(a, s, key0, page_of(a, s, key0, lane), lane);
-        int32_t page = page_of(a, s, key0 + 4 * TILE, lane);
+        int32_t key0 = s.first + TILE * wave, page = 0;
+        if (key0 < s.end) {
+            load(a, s, key0, page_of(a, s, key0, lane), lane);
+            page = page_of(a, s, key0 + WAVES * TILE, lane);
+        }
         while (key0 < s.end) {
             clear(a, lane);
             // values to LDS, as elements
@@ -264,10 +269,10 @@ struct Few {
             }
             const uint32_t there = valid;
             const int32_t now = key0;
-            key0 += 4 * TILE;
+            key0 += WAVES * TILE;
             if (key0 < s.end) {
                 load(a, s, key0, page, lane);
-                page = page_of(a, s, key0 + 4 * TILE, lane);
+                page = page_of(a, s, key0 + WAVES * TILE, lane);
             }
             if (there != 0xffffffffu || now + TILE - 1 > s.last0) {
                 const uint32_t mine_there = there >> (4 * g);   // this lane's keys, shifted so that each is a fixed bit
@@ -309,16 +314,16 @@ struct Few {
             __builtin_amdgcn_wave_barrier();
         }
 
-        // the four waves' results, joined
+        // the waves' results, joined
         l = other_half_sum(other_row_sum(l));
-        __shared__ float2 ml[4][ROWS];
+        __shared__ float2 ml[WAVES][ROWS];
         if (lane < 16) ml[wave][lane] = make_float2(m, l);
         __syncthreads();
         float best = kNone, sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) best = larger(best, ml[w][lane & 15].x);
+        for (int w = 0; w < WAVES; ++w) best = larger(best, ml[w][lane & 15].x);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float2 x = ml[w][lane & 15];
             if (x.x != kNone || x.y != x.y) sum += x.y * (x.x == kNone ? 1.0f : __builtin_amdgcn_exp2f((x.x - best) * a.c));
         }
@@ -332,16 +337,60 @@ struct Few {
             *reinterpret_cast<f32x4*>(join + (wave * ROWS + (lane & 15)) * OROW + 16 * t + 4 * g) = x;
         }
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
-        if (wave == 0 && lane < 16 && row.in)
-            at_global<float2>(a.part_ml)[s.part * rows + row.global] = make_float2(best == kNone ? kNone : best * a.c - kLift<DT>, sum);
+        const float most = best == kNone ? kNone : best * a.c - kLift<DT>;
+        __shared__ float weight[ROWS][kFinishSplits], own[ROWS], inverse[ROWS];
+        if (!a.finish) {
+            if (wave == 0 && lane < 16 && row.in) at_global<float2>(a.part_ml)[s.part * rows + row.global] = make_float2(most, sum);
+        } else {
+            // the rows' weights of the prefix's parts: a wave takes rows in turn, its lanes the parts
+            for (int r = wave; r < s.rows; r += WAVES) {
+                const int32_t global = row_of(a, s, r).global;
+                const float2 mine = make_float2(__shfl(most, r), __shfl(sum, r));
+                const float2 x = lane < a.prefix_splits ? at_global<const float2>(a.part_ml)[lane * rows + global] : make_float2(kNone, 0.0f);
+                float top = x.x;
+#pragma unroll
+                for (int i = 32; i; i >>= 1) top = larger(top, __shfl_xor(top, i));
+                top = larger(top, mine.x);
+                const float w = x.x == kNone ? 1.0f : __builtin_amdgcn_exp2f(x.x - top), w0 = mine.x == kNone ? 1.0f : __builtin_amdgcn_exp2f(mine.x - top);
+                float all = w * x.y;
+#pragma unroll
+                for (int i = 32; i; i >>= 1) all += __shfl_xor(all, i);
+                all += w0 * mine.y;
+                if (lane < kFinishSplits) weight[r][lane] = w;
+                if (lane == 0) {
+                    own[r] = w0;
+                    inverse[r] = all == 0.0f ? 0.0f : 1.0f / all;
+                    if (a.lse) at_global<float>(a.lse)[global] = lse_of(top, all);
+                }
+            }
+        }
         __syncthreads();
         for (int i = threadIdx.x; i < ROWS * DP / 4; i += THREADS) {
             const int r = i / (DP / 4), e = 4 * (i % (DP / 4));
             if (r >= s.rows || e >= a.d) continue;
+            const int32_t global = row_of(a, s, r).global;
             f32x4 x = *reinterpret_cast<const f32x4*>(join + r * OROW + e);
 #pragma unroll
-            for (int w = 1; w < 4; ++w) x += *reinterpret_cast<const f32x4*>(join + (w * ROWS + r) * OROW + e);
-            *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + (s.part * rows + row_of(a, s, r).global) * a.d + e) = x;
+            for (int w = 1; w < WAVES; ++w) x += *reinterpret_cast<const f32x4*>(join + (w * ROWS + r) * OROW + e);
+            if (!a.finish) {
+                *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + (s.part * rows + global) * a.d + e) = x;
+                continue;
+            }
+            x *= own[r];
+            const float* o = at_global<const float>(a.part_o) + static_cast<int64_t>(global) * a.d + e;
+            for (int32_t p = 0; p < a.prefix_splits; p += 8) {
+                f32x4 y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = *reinterpret_cast<const f32x4*>(o + min(p + j, a.prefix_splits - 1) * rows * a.d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (p + j < a.prefix_splits) x += weight[r][p + j] * y[j];
+            }
+            typedef T T4 __attribute__((ext_vector_type(4)));
+            T4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = static_cast<T>(x[j] * inverse[r]);
+            *reinterpret_cast<T4*>(at_global<T>(a.out) + static_cast<int64_t>(global) * a.d + e) = y;
         }
     }
 };
@@ -369,10 +418,6 @@ struct Many {
     static constexpr int BUF = TILE * (KROW + VROW) + TILE;     // keys, values, a byte for each key that is there
     static constexpr int LDS = 2 * BUF;
 
-    u32x4 k[NP], v[NP];
-    uint32_t k_scale[NP], v_scale[NP];
-    uint32_t valid;                                             // bit i: the key of piece i is there
-
     static __device__ __forceinline__ int key_of(int i) { return (THREADS / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
     static __device__ __forceinline__ int piece() { return static_cast<int>(threadIdx.x) % PIECES; }
 
@@ -381,54 +426,61 @@ struct Many {
 #pragma unroll
         for (int i = 0; i < NP; ++i) page[i] = s.table[min(key0 + key_of(i), s.end - 1) >> a.page_shift];
     }
-    __device__ __forceinline__ void load(const AttnArgs& a, const Share& s, int32_t key0, const int32_t (&page)[NP])
-    {
-        const int32_t row_bytes = a.d * ES, b = 16 * piece() < row_bytes ? 16 * piece() : 0;
-        valid = 0;
+    // What a thread stages of a tile: pieces on their way from memory, then written to LDS as elements.
+    struct Staged {
+        u32x4 k[NP], v[NP];
+        uint32_t k_scale[NP], v_scale[NP];
+        uint32_t valid;                                             // bit i: the key of piece i is there
+
+        __device__ __forceinline__ void load(const AttnArgs& a, const Share& s, int32_t key0, const int32_t (&page)[NP])
+        {
+            const int32_t row_bytes = a.d * ES, b = 16 * piece() < row_bytes ? 16 * piece() : 0;
+            valid = 0;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const bool there = key0 + key_of(i) < s.end && in_cache(a, page[i]);
-            valid |= there ? 1u << i : 0u;
-            const Place p = place_of(a, s.head, there ? page[i] : 0, key0 + key_of(i), row_bytes);
-            k[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.k_pages) + (p.bytes + b));
-            v[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.v_pages) + (p.bytes + b));
-            if constexpr (CODES) {
-                k_scale[i] = at_global<const uint8_t>(a.k_scale)[p.row];
-                v_scale[i] = at_global<const uint8_t>(a.v_scale)[p.row];
+            for (int i = 0; i < NP; ++i) {
+                const bool there = key0 + key_of(i) < s.end && in_cache(a, page[i]);
+                valid |= there ? 1u << i : 0u;
+                const Place p = place_of(a, s.head, there ? page[i] : 0, key0 + key_of(i), row_bytes);
+                k[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.k_pages) + (p.bytes + b));
+                v[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.v_pages) + (p.bytes + b));
+                if constexpr (CODES) {
+                    k_scale[i] = at_global<const uint8_t>(a.k_scale)[p.row];
+                    v_scale[i] = at_global<const uint8_t>(a.v_scale)[p.row];
+                }
             }
         }
-    }
-    // Zeros in the place of keys that are not there and of elements beyond the head.
-    __device__ __forceinline__ void clear(const AttnArgs& a)
-    {
-        const bool in = 16 * piece() < a.d * ES;
-        if (__all(in && valid == (1u << NP) - 1)) return;
+        // Zeros in the place of keys that are not there and of elements beyond the head.
+        __device__ __forceinline__ void clear(const AttnArgs& a)
+        {
+            const bool in = 16 * piece() < a.d * ES;
+            if (__all(in && valid == (1u << NP) - 1)) return;
 #pragma unroll
-        for (int i = 0; i < NP; ++i)
-            if (!in || !((valid >> i) & 1)) {
-                k[i] = v[i] = u32x4{0, 0, 0, 0};
-                k_scale[i] = v_scale[i] = 127;
-            }
-    }
-    __device__ __forceinline__ void stage(char* buf) const
-    {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            char* kt = buf + key_of(i) * KROW + (CODES ? 32 : 16) * piece();
-            char* vt = buf + TILE * KROW + key_of(i) * VROW + (CODES ? 32 : 16) * piece();
-            if constexpr (CODES) {
-                const float ks = scale_of(k_scale[i]), vs = scale_of(v_scale[i]);
-                reinterpret_cast<T8*>(kt)[0] = elements_of<DT>(k[i][0], k[i][1], ks);
-                reinterpret_cast<T8*>(kt)[1] = elements_of<DT>(k[i][2], k[i][3], ks);
-                reinterpret_cast<T8*>(vt)[0] = elements_of<DT>(v[i][0], v[i][1], vs);
-                reinterpret_cast<T8*>(vt)[1] = elements_of<DT>(v[i][2], v[i][3], vs);
-            } else {
-                *reinterpret_cast<u32x4*>(kt) = k[i];
-                *reinterpret_cast<u32x4*>(vt) = v[i];
-            }
-            if (piece() == 0) buf[TILE * (KROW + VROW) + key_of(i)] = static_cast<char>((valid >> i) & 1);
+            for (int i = 0; i < NP; ++i)
+                if (!in || !((valid >> i) & 1)) {
+                    k[i] = v[i] = u32x4{0, 0, 0, 0};
+                    k_scale[i] = v_scale[i] = 127;
+                }
         }
-    }
+        __device__ __forceinline__ void stage(char* buf) const
+        {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                char* kt = buf + key_of(i) * KROW + (CODES ? 32 : 16) * piece();
+                char* vt = buf + TILE * KROW + key_of(i) * VROW + (CODES ? 32 : 16) * piece();
+                if constexpr (CODES) {
+                    const float ks = scale_of(k_scale[i]), vs = scale_of(v_scale[i]);
+                    reinterpret_cast<T8*>(kt)[0] = elements_of<DT>(k[i][0], k[i][1], ks);
+                    reinterpret_cast<T8*>(kt)[1] = elements_of<DT>(k[i][2], k[i][3], ks);
+                    reinterpret_cast<T8*>(vt)[0] = elements_of<DT>(v[i][0], v[i][1], vs);
+                    reinterpret_cast<T8*>(vt)[1] = elements_of<DT>(v[i][2], v[i][3], vs);
+                } else {
+                    *reinterpret_cast<u32x4*>(kt) = k[i];
+                    *reinterpret_cast<u32x4*>(vt) = v[i];
+                }
+                if (piece() == 0) buf[TILE * (KROW + VROW) + key_of(i)] = static_cast<char>((valid >> i) & 1);
+            }
+        }
+    };
 
     static __device__ __forceinline__ A mul(T8 a, T8 b, A c)
     {
@@ -440,108 +492,155 @@ struct Many {
     {
         // lane = row, and one of 2 (WIDE) or 4 groups of keys or elements
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
-        int32_t page[NP];
-        int32_t key0 = s.first;
-        pages_of(a, s, key0, page);
         const Row row = row_of(a, s, RW * wave + r);
         const bool busy = RW * wave < s.rows;                   // waves without rows only help to stage
-        load(a, s, key0, page);
         T8 q[NC];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) q[c] = query_piece<DT>(a, row, KC * c + 8 * g);
         A o[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = A{};
         float m = kNone, l = 0.0f;
         const float lag = kLazy / a.c;
 
-        pages_of(a, s, key0 + TILE, page);
-        clear(a);
-        stage(lds);
-        __syncthreads();
-        for (int cur = 0; key0 < s.end; key0 += TILE, cur ^= 1) {
-            const bool more = key0 + TILE < s.end;
-            if (more) {
-                load(a, s, key0 + TILE, page);
-                pages_of(a, s, key0 + 2 * TILE, page);
+        const auto attend = [&](const char* buf, int32_t key0) {
+            const char* kt = buf + r * KROW + 16 * g;
+            A z[NS];
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                z[t] = A{};
+#pragma unroll
+                for (int c = 0; c < NC; ++c) z[t] = mul(*reinterpret_cast<const T8*>(kt + RW * t * KROW + 2 * KC * c), q[c], z[t]);
             }
-            const char* buf = lds + cur * BUF;
-            if (busy) {
-                const char* kt = buf + r * KROW + 16 * g;
-                A z[NS];
+            const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane % TILE] != 0) & full_of(TILE);
+            if (there != full_of(TILE) || key0 + TILE - 1 > s.last0) {
+                // this lane's keys, shifted so that each is a fixed bit (a mask made for every score would be held in registers)
+                const uint64_t mine = there >> (4 * g);
+                const int32_t last = row.last - key0 - 4 * g;
 #pragma unroll
-                for (int t = 0; t < NS; ++t) {
-                    z[t] = A{};
+                for (int t = 0; t < NS; ++t)
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) z[t] = mul(*reinterpret_cast<const T8*>(kt + RW * t * KROW + 2 * KC * c), q[c], z[t]);
-                }
-                const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane % TILE] != 0) & full_of(TILE);
-                if (there != full_of(TILE) || key0 + TILE - 1 > s.last0) {
-                    // this lane's keys, shifted so that each is a fixed bit (a mask made for every score would be held in registers)
-                    const uint64_t mine = there >> (4 * g);
-                    const int32_t last = row.last - key0 - 4 * g;
-#pragma unroll
-                    for (int t = 0; t < NS; ++t)
-#pragma unroll
-                        for (int i = 0; i < AN; ++i) {
-                            const int at = RW * t + (WIDE ? 8 * (i >> 2) : 0) + (i & 3);
-                            if (!((mine >> at) & 1) || at > last) z[t][i] = kNone;
-                        }
-                }
-                float top = z[0][0];
-#pragma unroll
-                for (int i = 1; i < NS * AN; ++i) top = larger(top, z[i / AN][i % AN]);
-                if constexpr (!WIDE) top = other_row_max(top);
-                top = other_half_max(top);
-                if (__any(top > m + lag)) {
-                    const float next = larger(m, top);
-                    const float down = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - next) * a.c);
-                    l *= down;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int i = 0; i < AN; ++i) o[t][i] *= down;
-                    m = next;
-                }
-                const float base = m == kNone ? 0.0f : m * a.c - kLift<DT>;
-                // where this lane's 8 bytes of a transposing read begin: of 4 keys, its (lane % 16) / 4 th, elements 4 (lane % 4) of 16
-                const char* vt = buf + TILE * KROW + (4 * g + ((lane & 15) >> 2)) * VROW + (WIDE ? 32 * ((lane >> 4) & 1) : 0) + 8 * (lane & 3);
-#pragma unroll
-                for (int u = 0; u < TILE / KC; ++u) {
-                    T8 p;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float x = WIDE ? z[u / 2][(8 * u + j) % AN] : z[2 * u + j / 4][j % 4];
-                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.c, -base));
-                        l += w;
-                        p[j] = static_cast<T>(w);
+                    for (int i = 0; i < AN; ++i) {
+                        const int at = RW * t + (WIDE ? 8 * (i >> 2) : 0) + (i & 3);
+                        if (!((mine >> at) & 1) || at > last) z[t][i] = kNone;
                     }
+            }
+            float top = z[0][0];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const char* at = vt + KC * u * VROW + 2 * RW * t;
-                        o[t] = mul(two_transposed<DT>(at, at + KC / 2 * VROW), p, o[t]);
-                    }
+            for (int i = 1; i < NS * AN; ++i) top = larger(top, z[i / AN][i % AN]);
+            if constexpr (!WIDE) top = other_row_max(top);
+            top = other_half_max(top);
+            if (__any(top > m + lag)) {
+                const float next = larger(m, top);
+                const float down = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - next) * a.c);
+                l *= down;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < AN; ++i) o[t][i] *= down;
+                m = next;
+            }
+            const float base = m == kNone ? 0.0f : m * a.c - kLift<DT>;
+            // where this lane's 8 bytes of a transposing read begin: of 4 keys, its (lane % 16) / 4 th, elements 4 (lane % 4) of 16
+            const char* vt = buf + TILE * KROW + (4 * g + ((lane & 15) >> 2)) * VROW + (WIDE ? 32 * ((lane >> 4) & 1) : 0) + 8 * (lane & 3);
+#pragma unroll
+            for (int u = 0; u < TILE / KC; ++u) {
+                T8 p;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = WIDE ? z[u / 2][(8 * u + j) % AN] : z[2 * u + j / 4][j % 4];
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.c, -base));
+                    l += w;
+                    p[j] = static_cast<T>(w);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const char* at = vt + KC * u * VROW + 2 * RW * t;
+                    o[t] = mul(two_transposed<DT>(at, at + KC / 2 * VROW), p, o[t]);
                 }
             }
-            if (more) {
-                clear(a);
-                stage(lds + (cur ^ 1) * BUF);
-            }
+        };
+
+        if (s.first < s.end) {
+            // Tiles are asked for two turns before they are staged (a turn is shorter than memory takes), in two sets of registers.
+            Staged even, odd;
+            int32_t page[NP];
+            pages_of(a, s, s.first, page);
+            even.load(a, s, s.first, page);
+            pages_of(a, s, s.first + TILE, page);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) q[c] = query_piece<DT>(a, row, KC * c + 8 * g);
+            if (s.first + TILE < s.end) odd.load(a, s, s.first + TILE, page);
+            pages_of(a, s, s.first + 2 * TILE, page);
+            even.clear(a);
+            even.stage(lds);
             __syncthreads();
+            // one turn: `key0`'s tile is in `buf`, the next one arrives in `next`, the one after is asked for into `after`
+            const auto turn = [&](int32_t key0, char* buf, char* other, Staged& next, Staged& after) {
+                if (key0 + 2 * TILE < s.end) {
+                    after.load(a, s, key0 + 2 * TILE, page);
+                    pages_of(a, s, key0 + 3 * TILE, page);
+                }
+                if (busy) attend(buf, key0);
+                if (key0 + TILE < s.end) {
+                    next.clear(a);
+                    next.stage(other);
+                }
+                __syncthreads();
+            };
+            for (int32_t key0 = s.first; key0 < s.end; key0 += 2 * TILE) {
+                turn(key0, lds, lds + BUF, odd, even);
+                if (key0 + TILE >= s.end) break;
+                turn(key0 + TILE, lds + BUF, lds, even, odd);
+            }
         }
         if (!busy) return;
         if constexpr (!WIDE) l = other_row_sum(l);
         l = other_half_sum(l);
         if (!row.in) return;
-        const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads, at = s.part * rows + row.global;
-        if (g == 0) at_global<float2>(a.part_ml)[at] = make_float2(m == kNone ? kNone : m * a.c - kLift<DT>, l);
+        const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
+        float most = m == kNone ? kNone : m * a.c - kLift<DT>;
+        if (!a.finish) {
+            const int64_t at = s.part * rows + row.global;
+            if (g == 0) at_global<float2>(a.part_ml)[at] = make_float2(most, l);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < AN / 4; ++i) {
+                    const int32_t e = RW * t + 8 * i + 4 * g;
+                    if (e < a.d)
+                        *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + at * a.d + e) = f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+                }
+            return;
+        }
+        // the prefix's parts, and the result
+        for (int32_t p = 0; p < a.prefix_splits; ++p) {
+            const int64_t at = p * rows + row.global;
+            const float2 x = at_global<const float2>(a.part_ml)[at];
+            const float next = larger(most, x.x);
+            const float mine = most == kNone ? 1.0f : __builtin_amdgcn_exp2f(most - next), its = x.x == kNone ? 1.0f : __builtin_amdgcn_exp2f(x.x - next);
+            most = next;
+            l = l * mine + x.y * its;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < AN / 4; ++i) {
+                    const int32_t e = RW * t + 8 * i + 4 * g;
+                    const f32x4 y = *reinterpret_cast<const f32x4*>(at_global<const float>(a.part_o) + at * a.d + (e < a.d ? e : 0));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[t][4 * i + j] = o[t][4 * i + j] * mine + y[j] * its;
+                }
+        }
+        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+        if (a.lse && g == 0) at_global<float>(a.lse)[row.global] = lse_of(most, l);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < AN / 4; ++i) {
                 const int32_t e = RW * t + 8 * i + 4 * g;
-                if (e < a.d)
-                    *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + at * a.d + e) = f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                T4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = static_cast<T>(o[t][4 * i + j] * inverse);
+                if (e < a.d) *reinterpret_cast<T4*>(at_global<T>(a.out) + static_cast<int64_t>(row.global) * a.d + e) = y;
             }
     }
 };
@@ -549,16 +648,19 @@ struct Many {
 // Workgroups of the prefix first, then those of the suffixes.  Workgroups go round the 8 XCDs; the row tiles of one head and
 // key range stand 8 apart, so that they read it through the same L2 at the same time.
 // FORM: see prefixattn_args.h.
-template <int DT, int FORMAT, int DP, int FORM> struct form;
-template <int DT, int FORMAT, int DP> struct form<DT, FORMAT, DP, FEW> { typedef Few<DT, FORMAT, DP> type; };
-template <int DT, int FORMAT, int DP> struct form<DT, FORMAT, DP, MANY_64> { typedef Many<DT, FORMAT, DP, 16, 4> type; };
-template <int DT, int FORMAT, int DP> struct form<DT, FORMAT, DP, MANY_128> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4)> type; };
+template <int DP> constexpr int threads_of(int form) { return form == MANY_256 || (form == MANY_128 && DP > 128) ? 512 : 256; }
+template <int DT, int FORMAT, int DP, int FORM, int WAVES> struct form;
+template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW, WAVES> { typedef Few<DT, FORMAT, DP, WAVES> type; };
+template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_64, WAVES> { typedef Many<DT, FORMAT, DP, 16, 4> type; };
+template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_128, WAVES> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4)> type; };
+template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8> type; };
 
 template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX>
-__global__ __launch_bounds__((form<DT, FORMAT, DP, PREFIX>::type::THREADS), 2) void attn_kernel(const AttnArgs a)
+__global__ __launch_bounds__(threads_of<DP>(PREFIX), 2) void attn_kernel(const AttnArgs a)
 {
-    typedef typename form<DT, FORMAT, DP, PREFIX>::type P;
-    typedef typename form<DT, FORMAT, DP, SUFFIX>::type S;
+    constexpr int WAVES = threads_of<DP>(PREFIX) / 64;          // few rows use all of them, whatever the prefix's form
+    typedef typename form<DT, FORMAT, DP, PREFIX, WAVES>::type P;
+    typedef typename form<DT, FORMAT, DP, SUFFIX, WAVES>::type S;
     __shared__ __attribute__((aligned(16))) char lds[P::LDS > S::LDS ? P::LDS : S::LDS];
     int32_t b = static_cast<int32_t>(blockIdx.x);
     Share s;
@@ -595,7 +697,7 @@ __global__ __launch_bounds__((form<DT, FORMAT, DP, PREFIX>::type::THREADS), 2) v
     s.end = min(s.first + a.suffix_chunk, keys);
     s.part = a.prefix_splits + split;
     s.last0 = keys - a.q_len;
-    if (s.first >= s.end) return;                               // the joining kernel knows the length, too
+    if (s.first >= s.end && !a.finish) return;                  // the joining kernel knows the length, too
     S().run(a, s, lds);
 }
 

@@ -7,7 +7,7 @@ namespace {
 template <int PREFIX, int SUFFIX>
 void launch(const AttnArgs& a, unsigned blocks, hipStream_t s)
 {
-    attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX, SUFFIX><<<blocks, form<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX>::type::THREADS, 0, s>>>(a);
+    attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX, SUFFIX><<<blocks, threads_of<UNIT_DP>(PREFIX), 0, s>>>(a);
 }
 
 }  // namespace
@@ -17,9 +17,18 @@ hipError_t ATTN_UNIT(UNIT_DT, UNIT_FORMAT, UNIT_DP)(const AttnArgs& a, int prefi
 {
     if (prefix_form == FEW) launch<FEW, FEW>(a, blocks, s);
     else if (prefix_form == MANY_64) suffix_form == FEW ? launch<MANY_64, FEW>(a, blocks, s) : launch<MANY_64, MANY_64>(a, blocks, s);
-    else if (suffix_form == FEW) launch<MANY_128, FEW>(a, blocks, s);
-    else if (suffix_form == MANY_64) launch<MANY_128, MANY_64>(a, blocks, s);
-    else launch<MANY_128, MANY_128>(a, blocks, s);
+    else if (prefix_form == MANY_128 || UNIT_DP != 128) {
+        if (suffix_form == FEW) launch<MANY_128, FEW>(a, blocks, s);
+        else if (suffix_form == MANY_64) launch<MANY_128, MANY_64>(a, blocks, s);
+        else launch<MANY_128, MANY_128>(a, blocks, s);
+    } else {
+#if UNIT_DP == 128
+        if (suffix_form == FEW) launch<MANY_256, FEW>(a, blocks, s);
+        else if (suffix_form == MANY_64) launch<MANY_256, MANY_64>(a, blocks, s);
+        else if (suffix_form == MANY_128) launch<MANY_256, MANY_128>(a, blocks, s);
+        else launch<MANY_256, MANY_256>(a, blocks, s);
+#endif
+    }
     return hipGetLastError();
 }
 

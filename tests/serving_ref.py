@@ -68,18 +68,19 @@ def attention(q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_len, s
 
     pre = places(prefix_pages, prefix_len) if prefix_len else []
     kp, vp = tokens(k_pages, k_scale, pre), tokens(v_pages, v_scale, pre)
-    for row in range(rows):
-        b, i = divmod(row, q_len)
+    for b in range(rows // q_len):
         width = 0 if suffix_pages is None else suffix_pages.shape[1] * page
         n = min(max(int(suffix_lens[b]), 0), width) if width else 0
-        seen = min(max(0, n - q_len + 1 + i), n)
-        at = places(suffix_pages[b], seen) if seen else []
+        at = places(suffix_pages[b], n) if n else []
+        here = [j for j in range(n) if 0 <= int(suffix_pages[b, j // page]) < pages] if n else []
         k, v = torch.cat((kp, tokens(k_pages, k_scale, at))), torch.cat((vp, tokens(v_pages, v_scale, at)))
-        for h in range(hq):
-            if k.shape[0]:
-                z = k[:, h // group] @ q[row, h].double() * scale
-                w = torch.softmax(z, 0)
-                lse[row, h] = torch.logsumexp(z, 0)
-                out[row, h] = w @ v[:, h // group]
-                size[row, h] = w @ v[:, h // group].abs()
+        for i in range(q_len):
+            row, end = b * q_len + i, len(pre) + sum(j <= n - q_len + i for j in here)
+            if end == 0:
+                continue
+            heads = torch.arange(hq) // group
+            kk, vv = k[:end, heads].transpose(0, 1), v[:end, heads].transpose(0, 1)          # [heads, keys, d]
+            z = (kk @ q[row].double()[:, :, None])[..., 0] * scale
+            w = torch.softmax(z, 1)[:, None]
+            lse[row], out[row], size[row] = torch.logsumexp(z, 1), (w @ vv)[:, 0], (w @ vv.abs())[:, 0]
     return out, lse, size

@@ -99,6 +99,16 @@ CASES = [
     (5, 2, 6, 3, 48, 1000, [1000, 0, 512, 513, 3], 250, 4, "fp16", False),
     (4, 1, 32, 8, 128, 2049, [1, 300, 0, 257], 10, 32, "bf16", True),
     (33, 1, 16, 4, 256, 260, [3] * 33, 1, 16, "fp16", False),
+    # batches that fill the chip with their suffixes: their workgroups join the prefix's parts
+    (130, 1, 8, 2, 128, 700, [(7 * i) % 41 - 1 for i in range(130)], 3, 16, "bf16", True),
+    (257, 1, 2, 1, 64, 0, [i % 5 for i in range(257)], 1, 4, "fp16", False),
+    (129, 2, 6, 2, 256, 33, [(5 * i) % 9 for i in range(129)], 2, 8, "bf16", False),
+    (64, 5, 16, 4, 128, 300, [(11 * i) % 50 for i in range(64)], 4, 16, "bf16", True),
+    (32, 5, 32, 8, 80, 0, [i for i in range(32)], 2, 16, "fp16", True),
+    (43, 13, 12, 2, 256, 130, [(3 * i) % 33 for i in range(43)], 3, 16, "fp16", False),
+    (65, 18, 16, 4, 96, 257, [(9 * i) % 40 for i in range(65)], 3, 16, "bf16", False),
+    (64, 25, 24, 4, 128, 65, [(13 * i) % 90 for i in range(64)], 6, 16, "bf16", True),
+    (86, 20, 21, 3, 64, 200, [(7 * i) % 60 for i in range(86)], 4, 16, "fp16", True),
 ]
 
 
