@@ -98,6 +98,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttnArgs a)
 
 constexpr int64_t kMaxBlocks = 1 << 24;      // of 256 threads: a launch has fewer than 2^32
 constexpr int32_t kMinChunk = 256;
+constexpr int64_t kInlineKeys = 512;         // up to here a prefix is seen by each suffix's workgroup, and there is one launch
 constexpr int64_t kFinishUnits = 256;        // from here on the suffixes alone fill the chip
 constexpr int64_t kJoinRows = 1024;          // from here on a wave joins a row: 4 waves a CU
 
@@ -159,6 +160,16 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
     // a CU holds one workgroup of eight waves, two of four that share keys, three of those with few rows
     auto wanted = [p](int form) { return form == FEW ? 768 : form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
+    if (a.pages && a.prefix_len && p->suffix_form == FEW && a.prefix_len <= kInlineKeys &&
+        (static_cast<int64_t>(a.kv_heads) * s->batch >= kFinishUnits || a.prefix_len + width <= 2 * kInlineKeys)) {
+        p->prefix_form = p->suffix_form;
+        p->finish = true;
+        a.inline_len = a.prefix_len;
+        a.suffix_tiles = a.suffix_splits = 1;
+        a.suffix_chunk = static_cast<int32_t>(width);
+        p->suffix_blocks = static_cast<int64_t>(a.kv_heads) * s->batch;
+        return p->suffix_blocks > kMaxBlocks ? fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)p->suffix_blocks) : ADDRMS_OK;
+    }
     if (a.prefix_len && a.pages) {
         a.prefix_tiles = static_cast<int32_t>(tiles(all, p->prefix_form));
         a.prefix_splits = splits_of(a.prefix_len, static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, wanted(p->prefix_form), &a.prefix_chunk);
@@ -210,9 +221,9 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
     if (!(scale > 0.0f) || !(scale < INFINITY)) return fail(ADDRMS_ERR_INVALID_ARG, "scale must be > 0 and finite (got %g)", static_cast<double>(scale));
     if (shape->batch == 0 || shape->q_len == 0) return ADDRMS_OK;
     AttnArgs& a = p.a;
-    const bool codes = shape->format == KVCACHE_E4M3, keys = a.prefix_splits || a.suffix_splits;
+    const bool codes = shape->format == KVCACHE_E4M3, keys = a.prefix_splits || a.suffix_splits, own = a.suffix_splits && shape->suffix_width;
     if (!q || !q_strides || !out || (keys && (!k_pages || !v_pages || (p.bytes && !workspace) || (codes && (!k_scale || !v_scale)))) ||
-        (a.prefix_splits && !prefix_pages) || (a.suffix_splits && (!suffix_pages || !suffix_lens)))
+        ((a.prefix_splits || a.inline_len) && !prefix_pages) || (own && (!suffix_pages || !suffix_lens)))
         return fail(ADDRMS_ERR_INVALID_ARG, "no pointer may be NULL");
     if (workspace_bytes < p.bytes)
         return fail(ADDRMS_ERR_INVALID_ARG, "the workspace has %lld bytes, the call needs %lld", (long long)workspace_bytes, (long long)p.bytes);
@@ -233,7 +244,7 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
     const AttnLaunch unit = kUnits[shape->dtype == ADDRMS_FP16][codes][p.dp == 64 ? 0 : p.dp == 128 ? 1 : 2];
     a.prefix_blocks = static_cast<int32_t>(p.prefix_blocks);
     if (p.finish) {
-        if (p.prefix_blocks) SERVING_HIP_TRY(unit(a, p.prefix_form, p.prefix_form == FEW ? FEW : p.suffix_form, static_cast<unsigned>(p.prefix_blocks), s));
+        if (p.prefix_blocks) SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.prefix_blocks), s));
         a.finish = 1;
         a.prefix_blocks = 0;
         SERVING_HIP_TRY(unit(a, p.suffix_form, p.suffix_form, static_cast<unsigned>(p.suffix_blocks), s));

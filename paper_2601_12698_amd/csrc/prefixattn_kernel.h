@@ -85,11 +85,17 @@ __device__ __forceinline__ float other_row_sum(float x) { const pair p = with_ro
 
 // A workgroup's share: rows [row0, row0 + rows) of a key head, rows counted token by token from token `token0`, keys
 // [first, end) of a table of pages.  Query i of its sequence sees keys up to last0 + i.
+// Keys from `turn` on are those of a second table, counted from 0 there (a short prefix, then a suffix; kAll: none).
 struct Share {
-    const int32_t* table;
-    int32_t head, token0, row0, rows, first, end, part, last0;
+    addr_t table, table2;
+    int32_t turn, head, token0, row0, rows, first, end, part, last0;
 };
 constexpr int32_t kAll = 1 << 30;
+__device__ __forceinline__ int32_t page_at(const AttnArgs& a, const Share& s, int32_t key)
+{
+    const bool second = key >= s.turn;
+    return at_global<const int32_t>(second ? s.table2 : s.table)[(second ? key - s.turn : key) >> a.page_shift];
+}
 
 struct Row {
     bool in;
@@ -104,7 +110,7 @@ __device__ __forceinline__ Row row_of(const AttnArgs& a, const Share& s, int32_t
     const int32_t at = s.row0 + (row.in ? r : 0);
     const int32_t i = at / a.group, head = s.head * a.group + (at - i * a.group), token = s.token0 + i;
     row.global = token * a.q_heads + head;
-    row.last = s.last0 + (s.last0 >= kAll ? 0 : i);
+    row.last = s.last0 >= kAll ? kAll : max(s.last0 + i, s.turn < kAll ? s.turn - 1 : -1);     // a prefix is seen whole, also by a query before its suffix
     row.q = token * a.q_token + head * a.q_head;
     return row;
 }
@@ -158,6 +164,8 @@ struct Few {
     uint32_t k_scale, v_scale;                                  // of key lane % 32
     uint32_t valid;                                             // keys of the tile that are there
 
+    static __device__ __forceinline__ int32_t local(const Share& s, int32_t key) { return key >= s.turn ? key - s.turn : key; }
+
     // `page` is that of key lane % 32.
     __device__ __forceinline__ void load(const AttnArgs& a, const Share& s, int32_t key0, int32_t page, int lane)
     {
@@ -166,7 +174,7 @@ struct Few {
         valid = static_cast<uint32_t>(__ballot(there));
         if (!there) page = 0;
         if constexpr (CODES) {
-            const uint64_t row = place_of(a, s.head, page, mine, 0).row;
+            const uint64_t row = place_of(a, s.head, page, local(s, mine), 0).row;
             k_scale = at_global<const uint8_t>(a.k_scale)[row];
             v_scale = at_global<const uint8_t>(a.v_scale)[row];
         }
@@ -176,7 +184,7 @@ struct Few {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int at = 16 * t + (lane & 15);
-            const char* r = kp + place_of(a, s.head, __shfl(page, at), key0 + at, row_bytes).bytes;
+            const char* r = kp + place_of(a, s.head, __shfl(page, at), local(s, key0 + at), row_bytes).bytes;
 #pragma unroll
             for (int c = 0; c < NK; ++c) {
                 const int32_t b = 64 * c + 16 * (lane >> 4);    // 16 bytes: 8 elements, or 16 codes
@@ -187,7 +195,7 @@ struct Few {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = (64 / PIECES) * i + lane / PIECES;
-            v[i] = *reinterpret_cast<const u32x4*>(vp + place_of(a, s.head, __shfl(page, at), key0 + at, row_bytes).bytes + (b < row_bytes ? b : 0));
+            v[i] = *reinterpret_cast<const u32x4*>(vp + place_of(a, s.head, __shfl(page, at), local(s, key0 + at), row_bytes).bytes + (b < row_bytes ? b : 0));
         }
     }
     // Zeros in the place of keys that are not there and of elements beyond the head.
@@ -208,10 +216,11 @@ struct Few {
 
     static __device__ __forceinline__ int32_t page_of(const AttnArgs& a, const Share& s, int32_t key0, int lane)
     {
-        return s.table[min(key0 + (lane & 31), s.end - 1) >> a.page_shift];
+        return page_at(a, s, min(key0 + (lane & 31), s.end - 1));
     }
 
-    __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, char* lds)
+    // `page0`: that of key lane % 32 of this wave's first tile.
+    __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, int32_t page0, char* lds)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
         const Row row = row_of(a, s, lane & 15);
@@ -232,7 +241,7 @@ struct Few {
 
         int32_t key0 = s.first + TILE * wave, page = 0;
         if (key0 < s.end) {
-            load(a, s, key0, page_of(a, s, key0, lane), lane);
+            load(a, s, key0, page0, lane);
             page = page_of(a, s, key0 + WAVES * TILE, lane);
         }
         while (key0 < s.end) {
@@ -424,7 +433,7 @@ struct Many {
     static __device__ __forceinline__ void pages_of(const AttnArgs& a, const Share& s, int32_t key0, int32_t (&page)[NP])
     {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) page[i] = s.table[min(key0 + key_of(i), s.end - 1) >> a.page_shift];
+        for (int i = 0; i < NP; ++i) page[i] = at_global<const int32_t>(s.table)[min(key0 + key_of(i), s.end - 1) >> a.page_shift];
     }
     // What a thread stages of a tile: pieces on their way from memory, then written to LDS as elements.
     struct Staged {
@@ -656,7 +665,7 @@ template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MAN
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8> type; };
 
 template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX>
-__global__ __launch_bounds__(threads_of<DP>(PREFIX), 2) void attn_kernel(const AttnArgs a)
+__global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW ? 1 : 2)) void attn_kernel(const AttnArgs a)
 {
     constexpr int WAVES = threads_of<DP>(PREFIX) / 64;          // few rows use all of them, whatever the prefix's form
     typedef typename form<DT, FORMAT, DP, PREFIX, WAVES>::type P;
@@ -664,12 +673,14 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), 2) void attn_kernel(const A
     __shared__ __attribute__((aligned(16))) char lds[P::LDS > S::LDS ? P::LDS : S::LDS];
     int32_t b = static_cast<int32_t>(blockIdx.x);
     Share s;
+    s.table2 = 0;
+    s.turn = kAll;
     if (b < a.prefix_blocks) {
         const int32_t j = b >> 3, tile = j % a.prefix_tiles, pair = (j / a.prefix_tiles) * 8 + (b & 7);
         if (pair >= a.prefix_splits * a.kv_heads) return;
         const int32_t split = pair / a.kv_heads;
         s.head = pair - split * a.kv_heads;
-        s.table = at_global<const int32_t>(a.prefix_pages);
+        s.table = a.prefix_pages;
         s.token0 = 0;
         s.row0 = tile * P::ROWS;
         s.rows = min(P::ROWS, a.batch * a.q_len * a.group - s.row0);
@@ -677,7 +688,8 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), 2) void attn_kernel(const A
         s.end = min(s.first + a.prefix_chunk, a.prefix_len);
         s.part = split;
         s.last0 = kAll;
-        P().run(a, s, lds);
+        if constexpr (PREFIX == FEW) P().run(a, s, P::page_of(a, s, s.first + P::TILE * (threadIdx.x >> 6), threadIdx.x & 63), lds);
+        else P().run(a, s, lds);
         return;
     }
     if (threadIdx.x >= S::THREADS) return;                      // a form with more waves than the suffixes' leaves the others idle
@@ -686,19 +698,36 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), 2) void attn_kernel(const A
     b -= seq * a.suffix_tiles * a.suffix_splits * a.kv_heads;
     const int32_t split = b / (a.suffix_tiles * a.kv_heads);
     b -= split * a.suffix_tiles * a.kv_heads;
-    const int32_t tile = b / a.kv_heads;
-    const int32_t keys = min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), a.suffix_width << a.page_shift);
+    const int32_t tile = b / a.kv_heads, room = a.suffix_width << a.page_shift;
     s.head = b - tile * a.kv_heads;
-    s.table = at_global<const int32_t>(a.suffix_pages) + static_cast<int64_t>(seq) * a.suffix_width;
     s.token0 = seq * a.q_len;
     s.row0 = tile * S::ROWS;
     s.rows = min(S::ROWS, a.q_len * a.group - s.row0);
-    s.first = split * a.suffix_chunk;
-    s.end = min(s.first + a.suffix_chunk, keys);
     s.part = a.prefix_splits + split;
-    s.last0 = keys - a.q_len;
-    if (s.first >= s.end && !a.finish) return;                  // the joining kernel knows the length, too
-    S().run(a, s, lds);
+    s.first = split * a.suffix_chunk;
+    s.table = a.suffix_pages + 4 * static_cast<int64_t>(seq) * a.suffix_width;
+    if constexpr (SUFFIX == FEW) {
+        if (a.inline_len) {
+            s.table2 = s.table;
+            s.table = a.prefix_pages;
+            s.turn = a.inline_len;
+        }
+        // The first tile's pages are asked for together with the length, as if the row of pages were full: a page number is checked
+        // before it is used, and what is beyond the length masked.
+        s.end = a.inline_len + room;
+        const int32_t page0 = s.first < s.end ? S::page_of(a, s, s.first + S::TILE * (threadIdx.x >> 6), threadIdx.x & 63) : 0;
+        const int32_t keys = room ? min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), room) : 0;
+        s.end = a.inline_len ? a.inline_len + keys : min(s.first + a.suffix_chunk, keys);
+        s.last0 = a.inline_len + keys - a.q_len;
+        if (s.first >= s.end && !a.finish) return;              // the joining kernel knows the length, too
+        S().run(a, s, page0, lds);
+    } else {
+        const int32_t keys = min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), room);
+        s.end = min(s.first + a.suffix_chunk, keys);
+        s.last0 = keys - a.q_len;
+        if (s.first >= s.end && !a.finish) return;
+        S().run(a, s, lds);
+    }
 }
 
 }  // namespace serving

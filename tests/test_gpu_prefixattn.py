@@ -99,6 +99,16 @@ CASES = [
     (5, 2, 6, 3, 48, 1000, [1000, 0, 512, 513, 3], 250, 4, "fp16", False),
     (4, 1, 32, 8, 128, 2049, [1, 300, 0, 257], 10, 32, "bf16", True),
     (33, 1, 16, 4, 256, 260, [3] * 33, 1, 16, "fp16", False),
+    # longer prefixes, seen by workgroups of their own: 16, 64, 128 and 256 rows
+    (40, 1, 4, 1, 128, 600, [i % 9 for i in range(40)], 2, 8, "bf16", False),
+    (9, 4, 4, 1, 64, 700, [0, 1, 2, 3, 4, 5, 33, 20, 7], 3, 16, "bf16", True),
+    (20, 1, 8, 2, 256, 900, [i % 11 for i in range(20)], 1, 16, "bf16", True),
+    (13, 1, 4, 1, 256, 577, [2] * 13, 1, 32, "fp16", False),
+    (70, 1, 4, 1, 128, 1100, [i % 40 for i in range(70)], 3, 16, "fp16", True),
+    (70, 1, 4, 1, 96, 1100, [i % 40 for i in range(70)], 3, 16, "bf16", False),
+    (24, 1, 5, 1, 112, 777, [i % 5 for i in range(24)], 1, 64, "bf16", False),
+    (30, 1, 5, 1, 48, 3000, [i % 5 for i in range(30)], 1, 64, "fp16", True),
+    (3, 1, 5, 1, 128, 5000, [100, 0, 1700], 30, 64, "bf16", True),
     # batches that fill the chip with their suffixes: their workgroups join the prefix's parts
     (130, 1, 8, 2, 128, 700, [(7 * i) % 41 - 1 for i in range(130)], 3, 16, "bf16", True),
     (257, 1, 2, 1, 64, 0, [i % 5 for i in range(257)], 1, 4, "fp16", False),
@@ -122,7 +132,7 @@ def test_against_64_bits(case):
 
 
 def test_pages_outside_the_cache_are_masked():
-    for case in (CASES[3], CASES[7], CASES[10]):
+    for case in (CASES[3], CASES[7], CASES[10], CASES[17], CASES[18], CASES[19], CASES[20], CASES[21]):
         c, dtype = build(case, seed=3)
         c["prefix_pages"][1] = -1
         c["prefix_pages"][-1] = c["k_pages"].shape[0]
@@ -152,10 +162,10 @@ def test_no_keys_at_all_and_no_tokens():
 
 
 @pytest.mark.parametrize("quantised", [False, True])
-@pytest.mark.parametrize("batch", [1, 40])
-def test_large_scores_and_a_late_maximum(quantised, batch):
+@pytest.mark.parametrize("batch,prefix", [(1, 400), (1, 640), (40, 640), (70, 640)])
+def test_large_scores_and_a_late_maximum(quantised, batch, prefix):
     """Scores that grow from key to key by far more than an exponent holds, and one key that has nearly all the weight at the end."""
-    c, dtype = build((batch, 1, 4, 1, 64, 640, [3] * batch, 1, 16, "bf16", quantised), seed=6, junk=False)
+    c, dtype = build((batch, 1, 4, 1, 128, prefix, [3] * batch, 1, 16, "bf16", quantised), seed=6, junk=False)
     c["scale"] = 3.0
     check(c, dtype, call(c, dtype))
     c["scale"] = 40.0
@@ -165,8 +175,9 @@ def test_large_scores_and_a_late_maximum(quantised, batch):
     check(c, dtype, got)
 
 
-def test_nan_in_a_seen_key_reaches_its_row_alone():
-    c, dtype = build((20, 1, 4, 2, 64, 100, [5] * 20, 1, 16, "bf16", False), seed=7)
+@pytest.mark.parametrize("prefix", [100, 800])
+def test_nan_in_a_seen_key_reaches_its_row_alone(prefix):
+    c, dtype = build((20, 1, 4, 2, 64, prefix, [5] * 20, 1, 16, "bf16", False), seed=7)
     p = int(c["suffix_pages"][3, 0])
     c["v_pages"][p, 1, 2, 5] = math.nan
     out, lse = call(c, dtype)
@@ -182,7 +193,7 @@ def test_nan_in_a_seen_key_reaches_its_row_alone():
 def test_split_states_merge_to_the_same_result():
     """out and lse are what mergestates_run takes: prefix alone and suffixes alone, merged, are the whole."""
     from paper_2601_12698_amd import binding as B
-    c, dtype = build((6, 1, 8, 2, 128, 333, [9, 1, 30, 4, 16, 17], 2, 16, "bf16", True), seed=8)
+    c, dtype = build((6, 1, 8, 2, 128, 1333, [9, 1, 30, 4, 16, 17], 2, 16, "bf16", True), seed=8)
     whole = call(c, dtype)
     a = call(dict(c, suffix_pages=None, suffix_lens=None), dtype)
     b = call(dict(c, prefix_len=0), dtype)
@@ -213,15 +224,17 @@ def test_a_cache_beyond_32_bits():
     check(c, "bf16", (out.cpu(), lse.cpu()))
 
 
-def test_on_another_stream_and_in_a_graph_with_growing_suffixes():
-    c, dtype = build((5, 1, 8, 2, 128, 150, [64] * 5, 4, 16, "bf16", True), seed=9)
+@pytest.mark.parametrize("short", [True, False])
+def test_on_another_stream_and_in_a_graph_with_growing_suffixes(short):
+    prefix = 150 if short else 1150
+    c, dtype = build((5, 1, 8, 2, 128, prefix, [64] * 5, 4, 16, "bf16", True), seed=9)
     dev = {n: x.cuda() if isinstance(x, torch.Tensor) else x for n, x in c.items()}
-    shape = S.prefixattn_shape(5, 1, 8, 2, 128, 16, c["k_pages"].shape[0], 150, 4, dtype, True)
+    shape = S.prefixattn_shape(5, 1, 8, 2, 128, 16, c["k_pages"].shape[0], prefix, 4, dtype, True)
     room = torch.empty(S.prefixattn_workspace_bytes(shape), dtype=torch.uint8, device="cuda")
     out, lse = torch.zeros((5, 8, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((5, 8), device="cuda")
 
     def step(o, s, **more):
-        S.prefixattn_run(dev["q"], dev["k_pages"], dev["v_pages"], dev["k_scale"], dev["v_scale"], dev["prefix_pages"], 150, dev["suffix_pages"],
+        S.prefixattn_run(dev["q"], dev["k_pages"], dev["v_pages"], dev["k_scale"], dev["v_scale"], dev["prefix_pages"], prefix, dev["suffix_pages"],
                          dev["suffix_lens"], o, s, c["scale"], dtype, workspace=room, **more)
 
     stream = torch.cuda.Stream()
@@ -243,8 +256,8 @@ def test_on_another_stream_and_in_a_graph_with_growing_suffixes():
 
 
 def test_one_workspace_after_the_other_and_refused_where_small():
-    c, dtype = build(CASES[2], seed=1)
-    shape = S.prefixattn_shape(2, 1, 8, 2, 128, 16, c["k_pages"].shape[0], 37, 1, dtype, True)
+    c, dtype = build((2, 1, 8, 2, 128, 600, [5, 16], 1, 16, "bf16", True), seed=1)
+    shape = S.prefixattn_shape(2, 1, 8, 2, 128, 16, c["k_pages"].shape[0], 600, 1, dtype, True)
     n = S.prefixattn_workspace_bytes(shape)
     with pytest.raises(S.AddrmsError, match="workspace has"):
         call(c, dtype, workspace=torch.empty(n - 1, dtype=torch.uint8, device="cuda"))

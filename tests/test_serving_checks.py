@@ -72,7 +72,7 @@ def test_cache_refusals(call, what, status):
 
 
 def shape(**more):
-    s = dict(batch=4, q_len=1, q_heads=8, kv_heads=2, d=128, page_size=16, pages=100, prefix_len=300, suffix_width=4, dtype="bf16", quantised=True)
+    s = dict(batch=4, q_len=1, q_heads=8, kv_heads=2, d=128, page_size=16, pages=100, prefix_len=3000, suffix_width=4, dtype="bf16", quantised=True)
     s.update(more)
     return S.prefixattn_shape(**s)
 
@@ -121,11 +121,14 @@ def test_attention_without_work_and_unknown_shapes():
 
 def test_workspace_holds_a_part_for_each_split():
     """4 d + 8 bytes for each row and part; the parts of a range never hold less than 256 keys but for the last.  Suffixes that fill
-    the chip by themselves join the prefix's parts to their own and have none."""
+    the chip by themselves join the prefix's parts to their own and have none, and where they also see a short prefix there is no part."""
     for prefix, width in ((0, 4), (1, 0), (256, 0), (257, 4), (100000, 100), (1 << 20, 1 << 10)):
         for batch, q_len, heads in ((1, 1, (1, 1)), (64, 1, (64, 8)), (3, 40, (8, 2))):
             s = shape(batch=batch, q_len=q_len, q_heads=heads[0], kv_heads=heads[1], prefix_len=prefix, suffix_width=width, pages=1 << 20)
             rows, n = batch * q_len * heads[0], S.prefixattn_workspace_bytes(s)
+            if n == 0:
+                assert prefix <= 512 and q_len * heads[0] // heads[1] <= 16
+                continue
             assert n % (rows * (4 * 128 + 8)) == 0
             parts = n // (rows * (4 * 128 + 8))
             assert (prefix > 0) + (width > 0 and batch * heads[1] < 256) <= parts <= -(-prefix // 256) + -(-width * 16 // 256)
@@ -135,7 +138,7 @@ def test_bytes_formulas():
     assert S.rotary_algorithmic_bytes(10, 5, 64, 3, "bf16") == 10 * (2 * 5 * 64 * 2 + 24)
     assert S.kvcache_algorithmic_bytes(10, 2, 64, "fp16") == 40 * 64 * 2 + 40 * 65 + 80
     assert S.kvcache_algorithmic_bytes(10, 2, 64, "fp16", quantised=False) == 40 * 64 * 4 + 80
-    assert S.prefixattn_algorithmic_bytes(shape(), 50) == 350 * 2 * 2 * 129 + 32 * (4 * 128 + 4)
+    assert S.prefixattn_algorithmic_bytes(shape(), 50) == 3050 * 2 * 2 * 129 + 32 * (4 * 128 + 4)
     with pytest.raises(E):
         S.rotary_algorithmic_bytes(10, 5, 64, 3, "fp16_res32")
 
