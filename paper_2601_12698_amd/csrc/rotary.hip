@@ -16,7 +16,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxTurns = 2048;              // angles of one workgroup: 16 KiB of LDS
-constexpr int kAhead = 4;                    // pieces of a thread that are under way together
+constexpr int kAhead = 2;                    // pieces of a thread that are under way together (8191 x 40 x 128 bf16: 2 38.5 us, 4 42.5, 8 48)
+constexpr int64_t kPastBytes = 4 << 20;      // of output: the L2 of one XCD
 
 struct RotaryArgs {
     addr_t q, k, q_out, k_out, positions, inv_freq, pair_axis;
@@ -43,12 +44,20 @@ __device__ __forceinline__ float2 turn_of(double r)
     return make_float2((which == 1 || which == 2) ? -a : a, which >= 2 ? -b : b);
 }
 
+template <bool PAST, typename T, typename P>
+__device__ __forceinline__ void put(T* p, P v)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<P*>(p));
+    else *reinterpret_cast<P*>(p) = v;
+}
+
 // V elements as one access of V * sizeof(T) bytes.
 template <typename T, int V> struct piece { typedef T type __attribute__((ext_vector_type(V))); };
 
-// A piece is V pairs: the elements [j, j + V) and [j + pairs, j + pairs + V), or with INTER the 2 V elements from 2 j on.
-// blockDim.x = pieces of a head (V pairs, or V elements that are copied), blockDim.y = heads side by side.
-template <int DT, int V, bool INTER>
+// A piece is V pairs, the elements [j, j + V) and [j + pairs, j + pairs + V), or with INTER the V / 2 pairs of the V elements from
+// 2 j on (V = 1: one pair, both elements).  blockDim.x = pieces of a head (pairs, or V elements that are copied), blockDim.y = heads
+// side by side.  PAST: outputs are written past the caches.
+template <int DT, int V, bool INTER, bool PAST>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a)
 {
     typedef typename elem<DT>::type T;
@@ -62,8 +71,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a)
     const int32_t px = static_cast<int32_t>(threadIdx.x), step = static_cast<int32_t>(blockDim.y);
     const bool turned = px < a.pair_pieces;
     // where this thread's piece of a head begins, and its second half
-    const int32_t e0 = turned ? (INTER ? 2 * V : V) * px : 2 * a.pairs + V * (px - a.pair_pieces);
-    const int32_t e1 = turned ? (INTER ? e0 + V : e0 + a.pairs) : e0;
+    constexpr bool SECOND = !INTER || V == 1;        // a piece has a second half
+    const int32_t e0 = turned ? (INTER && V == 1 ? 2 : V) * px : 2 * a.pairs + V * (px - a.pair_pieces);
+    const int32_t e1 = turned ? (INTER ? e0 + 1 : e0 + a.pairs) : e0;
 
     uint32_t at = threadIdx.y;                       // of the tokens' heads, one token's behind the other's
     bool first = true;
@@ -80,7 +90,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a)
                 const T* p = at_global<const T>(is_k ? a.k : a.q) + (t0 + tt[i]) * (is_k ? a.ks[0] : a.qs[0]) +
                              static_cast<int64_t>(is_k ? hh[i] - a.q_heads : hh[i]) * (is_k ? a.ks[1] : a.qs[1]);
                 x[i] = *reinterpret_cast<const P*>(p + e0);
-                if (turned) y[i] = *reinterpret_cast<const P*>(p + e1);
+                if (SECOND && turned) y[i] = *reinterpret_cast<const P*>(p + e1);
             }
         }
         if (first) {
@@ -104,12 +114,16 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a)
             T* p = at_global<T>(is_k ? a.k_out : a.q_out) + (t0 + tt[i]) * (is_k ? a.kos[0] : a.qos[0]) +
                    static_cast<int64_t>(is_k ? hh[i] - a.q_heads : hh[i]) * (is_k ? a.kos[1] : a.qos[1]);
             if (turned) {
-                const float2* cs = turns + tt[i] * a.pairs + px * V;
-                T in[2 * V], out[2 * V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) { in[j] = x[i][j]; in[V + j] = y[i][j]; }
+                constexpr int N = SECOND ? V : V / 2;       // pairs of the piece
+                const float2* cs = turns + tt[i] * a.pairs + px * N;
+                T in[2 * N], out[2 * N];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
+                    in[j] = x[i][j];
+                    if (SECOND) in[V + j] = y[i][j];
+                }
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
                     const int lo = INTER ? 2 * j : j, hi = INTER ? 2 * j + 1 : V + j;
                     const float u = static_cast<float>(in[lo]), v = static_cast<float>(in[hi]);
                     const float2 w = cs[j];
@@ -117,19 +131,22 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a)
                     out[hi] = static_cast<T>(__builtin_fmaf(u, w.y, v * w.x));
                 }
 #pragma unroll
-                for (int j = 0; j < V; ++j) { x[i][j] = out[j]; y[i][j] = out[V + j]; }
-                *reinterpret_cast<P*>(p + e1) = y[i];
+                for (int j = 0; j < V; ++j) {
+                    x[i][j] = out[j];
+                    if (SECOND) y[i][j] = out[V + j];
+                }
+                if (SECOND) put<PAST>(p + e1, y[i]);
             }
-            *reinterpret_cast<P*>(p + e0) = x[i];
+            put<PAST>(p + e0, x[i]);
         }
     }
 }
 
 template <int DT, int V>
-hipError_t launch(const RotaryArgs& a, bool inter, dim3 grid, dim3 block, hipStream_t s)
+hipError_t launch(const RotaryArgs& a, bool inter, bool past, dim3 grid, dim3 block, hipStream_t s)
 {
-    if (inter) rotary_kernel<DT, V, true><<<grid, block, 0, s>>>(a);
-    else rotary_kernel<DT, V, false><<<grid, block, 0, s>>>(a);
+    if (inter) past ? rotary_kernel<DT, V, true, true><<<grid, block, 0, s>>>(a) : rotary_kernel<DT, V, true, false><<<grid, block, 0, s>>>(a);
+    else past ? rotary_kernel<DT, V, false, true><<<grid, block, 0, s>>>(a) : rotary_kernel<DT, V, false, false><<<grid, block, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -186,7 +203,7 @@ int rotary_run(const void* q, const int64_t* q_strides, const void* k, const int
     bits |= static_cast<uint64_t>(a.pairs | (d - rot)) * es;
     // Pieces of 16 bytes where everything is a multiple of that, of 8 where it is of that, single elements else.
     const int v = bits % 16 == 0 ? 16 / es : bits % 8 == 0 && es == 2 ? 4 : 1;
-    a.pair_pieces = a.pairs / v;
+    a.pair_pieces = inter && v > 1 ? 2 * a.pairs / v : a.pairs / v;
     a.pieces = a.pair_pieces + (d - rot) / v;
     // A workgroup is as many heads side by side as 256 threads hold; each thread has about kAhead pieces, of several tokens where
     // their heads alone do not give them.  Few tokens: one a workgroup, and their heads over several, until there are 2 workgroups a CU.
@@ -201,13 +218,17 @@ int rotary_run(const void* q, const int64_t* q_strides, const void* k, const int
     const int64_t groups = (tokens + per - 1) / per;
     if (groups < many && a.heads > iy) a.heads_per_wg = iy;
     const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((a.heads + a.heads_per_wg - 1) / a.heads_per_wg)), block(ix, iy);
+    // Outputs that the L2s would not keep for the next kernel go past them where every store fills its 16-byte pieces' lines (8191
+    // tokens x 40 heads x 128 bf16 38.5 -> 32.5 us, 2048 x 40 x 96 fp32 13.9 -> 11.3, 1000 x 40 x 128 bf16 6.8 -> 5.8; 200 tokens, 2 MB,
+    // 3.6 either way).  Loads that go past them, too, gain 2 % at the largest and lose a quarter at the others.
+    const bool past = v * es == 16 && tokens * a.heads * static_cast<int64_t>(d) * es >= kPastBytes;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e;
-    if (dtype == ADDRMS_FP32) e = v == 4 ? launch<DT_FP32, 4>(a, inter, grid, block, s) : launch<DT_FP32, 1>(a, inter, grid, block, s);
+    if (dtype == ADDRMS_FP32) e = v == 4 ? launch<DT_FP32, 4>(a, inter, past, grid, block, s) : launch<DT_FP32, 1>(a, inter, past, grid, block, s);
     else if (dtype == ADDRMS_BF16)
-        e = v == 8 ? launch<DT_BF16, 8>(a, inter, grid, block, s) : v == 4 ? launch<DT_BF16, 4>(a, inter, grid, block, s) : launch<DT_BF16, 1>(a, inter, grid, block, s);
+        e = v == 8 ? launch<DT_BF16, 8>(a, inter, past, grid, block, s) : v == 4 ? launch<DT_BF16, 4>(a, inter, past, grid, block, s) : launch<DT_BF16, 1>(a, inter, past, grid, block, s);
     else
-        e = v == 8 ? launch<DT_FP16, 8>(a, inter, grid, block, s) : v == 4 ? launch<DT_FP16, 4>(a, inter, grid, block, s) : launch<DT_FP16, 1>(a, inter, grid, block, s);
+        e = v == 8 ? launch<DT_FP16, 8>(a, inter, past, grid, block, s) : v == 4 ? launch<DT_FP16, 4>(a, inter, past, grid, block, s) : launch<DT_FP16, 1>(a, inter, past, grid, block, s);
     if (e != hipSuccess) return fail(ADDRMS_ERR_HIP, "the launch failed: %s", hipGetErrorString(e));
     return ADDRMS_OK;
 }
