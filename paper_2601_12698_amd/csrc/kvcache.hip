@@ -1,9 +1,12 @@
 // Writing tokens into a paged cache, quantised, and reading them back (include/kvcache.h).
 //
 // A row is one head of one token.  Both kernels move each byte once and are bound by that.
-//   write: a row is read as pieces of 8 elements by 2 to 32 neighbouring lanes, which find its largest magnitude with lane
-//          exchanges, so that a row is read once and stays in registers; keys and values go together.
-//   read:  pieces of 16 elements: one 16-byte load of codes, two 16-byte stores.
+// A row is 2 to 32 neighbouring lanes of 8 elements each, keys and values together.  A row that is written stays in registers: its
+// lanes find the largest magnitude by exchanges and then round.  (A lane of 16 elements loads 16 bytes of codes at once, but then
+// its two stores of 16 bytes each fill every other half line: 131072 tokens x 8 x 128 bf16 165 us, with 8 elements 146.)
+// Results beyond an L2 go past the caches: 131072 tokens read back 146 -> 138 us, 16384 22.5 -> 17.3 (5.8 TB/s), 4999 x 4 x 256 fp16
+// 6.5 -> 6.4; written, 16384 x 8 x 128 23.2 -> 20.2 us, 4999 x 4 x 256 8.5 -> 7.9, 131072 151 -> 148; 64 tokens 2.7 either way.
+// Loads that go past them lose 2 to 20 %.
 #include "kvcache.h"
 #include "serving_internal.h"
 
@@ -13,6 +16,7 @@ using namespace serving;
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kPastBytes = 4 << 20;      // of keys and values in 16 bits: the L2 of one XCD
 
 struct CacheArgs {
     addr_t k, v, slots, k_pages, v_pages, k_scale, v_scale;
@@ -20,6 +24,13 @@ struct CacheArgs {
     int64_t ks[2], vs[2];                    // strides of k and v: token, head
     uint32_t heads, d, lanes_log2, page_shift;
 };
+
+template <bool PAST, typename P>
+__device__ __forceinline__ void put(P* p, P v)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
 
 // Row of the cache that a slot's head is: pages are [heads][page_size].
 __device__ __forceinline__ int64_t cache_row(int64_t slot, uint32_t head, const CacheArgs& a)
@@ -51,7 +62,7 @@ __device__ __forceinline__ vec8<DT> load8(const typename elem<DT>::type* p, bool
     return raw;
 }
 
-template <int DT>
+template <int DT, bool PAST>
 __device__ __forceinline__ void quantise(vec8<DT> raw, bool in, uint32_t lanes, bool first, char* codes, uint8_t* scale)
 {
     // the largest magnitude of four significant bits that the type holds
@@ -76,18 +87,18 @@ __device__ __forceinline__ void quantise(vec8<DT> raw, bool in, uint32_t lanes, 
         w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2] * inverse, x[4 * j + 3] * inverse, w, true);
         out[j] = static_cast<uint32_t>(w);
     }
-    if (in) *reinterpret_cast<u32x2*>(codes) = out;
+    if (in) put<PAST>(reinterpret_cast<u32x2*>(codes), out);
     if (first) *scale = static_cast<uint8_t>(s);
 }
 
-template <int DT, int FORMAT, bool WIDE>
+template <int DT, int FORMAT, bool WIDE, bool PAST>
 __global__ __launch_bounds__(kThreads) void write_kernel(const CacheArgs a)
 {
     typedef typename elem<DT>::type T;
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
     if (row >= a.rows) return;                                       // all lanes of a row together
-    const int64_t t = static_cast<int64_t>(static_cast<uint64_t>(row) / a.heads);
+    const int64_t t = static_cast<int64_t>(static_cast<uint32_t>(row) / a.heads);
     const uint32_t h = static_cast<uint32_t>(row - t * a.heads);
     const bool in = 8 * lane < a.d;
     const int64_t slot = at_global<const int64_t>(a.slots)[t];
@@ -97,58 +108,70 @@ __global__ __launch_bounds__(kThreads) void write_kernel(const CacheArgs a)
     const int64_t to = cache_row(slot, h, a);
     if constexpr (FORMAT == KVCACHE_E4M3) {
         const int64_t at = to * a.d + 8 * lane;
-        quantise<DT>(k, in, lanes, lane == 0, at_global<char>(a.k_pages) + at, at_global<uint8_t>(a.k_scale) + to);
-        quantise<DT>(v, in, lanes, lane == 0, at_global<char>(a.v_pages) + at, at_global<uint8_t>(a.v_scale) + to);
+        quantise<DT, PAST>(k, in, lanes, lane == 0, at_global<char>(a.k_pages) + at, at_global<uint8_t>(a.k_scale) + to);
+        quantise<DT, PAST>(v, in, lanes, lane == 0, at_global<char>(a.v_pages) + at, at_global<uint8_t>(a.v_scale) + to);
     } else if (in) {
-        *reinterpret_cast<vec8<DT>*>(at_global<T>(a.k_pages) + to * a.d + 8 * lane) = k;
-        *reinterpret_cast<vec8<DT>*>(at_global<T>(a.v_pages) + to * a.d + 8 * lane) = v;
+        put<PAST>(reinterpret_cast<vec8<DT>*>(at_global<T>(a.k_pages) + to * a.d + 8 * lane), k);
+        put<PAST>(reinterpret_cast<vec8<DT>*>(at_global<T>(a.v_pages) + to * a.d + 8 * lane), v);
     }
 }
 
+// Eight elements of a row as they are read back.
 template <int DT, int FORMAT>
-__device__ __forceinline__ void read16(addr_t pages, addr_t scales, int64_t from, bool kept, uint32_t e0, const CacheArgs& a, addr_t out, int64_t row)
-{
-    typedef typename elem<DT>::type T;
-    typedef vec8<DT> T8;
-    T8 x[2] = {};
-    if (kept) {
+struct Piece {
+    u32x2 codes;
+    vec8<DT> same;
+    uint32_t scale;
+
+    __device__ __forceinline__ void load(addr_t pages, addr_t scales, int64_t from, uint32_t e, const CacheArgs& a)
+    {
         if constexpr (FORMAT == KVCACHE_E4M3) {
-            const u32x4 codes = *reinterpret_cast<const u32x4*>(at_global<const char>(pages) + from * a.d + e0);
-            const uint32_t s = at_global<const uint8_t>(scales)[from];
-            const float scale = s ? __builtin_bit_cast(float, s << 23) : 0x1p-127f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes[j]), false);
-                const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes[j]), true);
-                x[j / 2][4 * (j & 1)] = static_cast<T>(lo[0] * scale);
-                x[j / 2][4 * (j & 1) + 1] = static_cast<T>(lo[1] * scale);
-                x[j / 2][4 * (j & 1) + 2] = static_cast<T>(hi[0] * scale);
-                x[j / 2][4 * (j & 1) + 3] = static_cast<T>(hi[1] * scale);
-            }
+            codes = *reinterpret_cast<const u32x2*>(at_global<const char>(pages) + from * a.d + e);
+            scale = at_global<const uint8_t>(scales)[from];
         } else {
-            const T8* p = reinterpret_cast<const T8*>(at_global<const T>(pages) + from * a.d + e0);
-            x[0] = p[0];
-            x[1] = p[1];
+            same = *reinterpret_cast<const vec8<DT>*>(at_global<const typename elem<DT>::type>(pages) + from * a.d + e);
         }
     }
-    T8* o = reinterpret_cast<T8*>(at_global<T>(out) + row * a.d + e0);
-    o[0] = x[0];
-    o[1] = x[1];
-}
+    __device__ __forceinline__ vec8<DT> values() const
+    {
+        typedef typename elem<DT>::type T;
+        if constexpr (FORMAT != KVCACHE_E4M3) return same;
+        vec8<DT> x;
+        const float by = scale ? __builtin_bit_cast(float, scale << 23) : 0x1p-127f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes[j]), false);
+            const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes[j]), true);
+            x[4 * j] = static_cast<T>(lo[0] * by);
+            x[4 * j + 1] = static_cast<T>(lo[1] * by);
+            x[4 * j + 2] = static_cast<T>(hi[0] * by);
+            x[4 * j + 3] = static_cast<T>(hi[1] * by);
+        }
+        return x;
+    }
+};
 
-template <int DT, int FORMAT>
+template <int DT, int FORMAT, bool PAST>
 __global__ __launch_bounds__(kThreads) void read_kernel(const CacheArgs a)
 {
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
-    if (row >= a.rows || 16 * lane >= a.d) return;
-    const int64_t t = static_cast<int64_t>(static_cast<uint64_t>(row) / a.heads);
+    if (row >= a.rows || 8 * lane >= a.d) return;
+    const int64_t t = static_cast<int64_t>(static_cast<uint32_t>(row) / a.heads);
     const uint32_t h = static_cast<uint32_t>(row - t * a.heads);
     const int64_t slot = at_global<const int64_t>(a.slots)[t];
-    const bool kept = slot >= 0 && slot < a.cache_slots;
-    const int64_t from = kept ? cache_row(slot, h, a) : 0;
-    read16<DT, FORMAT>(a.k_pages, a.k_scale, from, kept, 16 * lane, a, a.k, row);
-    read16<DT, FORMAT>(a.v_pages, a.v_scale, from, kept, 16 * lane, a, a.v, row);
+    vec8<DT> k = {}, v = {};
+    if (slot >= 0 && slot < a.cache_slots) {
+        const int64_t from = cache_row(slot, h, a);
+        Piece<DT, FORMAT> kp, vp;
+        kp.load(a.k_pages, a.k_scale, from, 8 * lane, a);
+        vp.load(a.v_pages, a.v_scale, from, 8 * lane, a);
+        k = kp.values();
+        v = vp.values();
+    }
+    typedef typename elem<DT>::type T;
+    put<PAST>(reinterpret_cast<vec8<DT>*>(at_global<T>(a.k) + row * a.d + 8 * lane), k);
+    put<PAST>(reinterpret_cast<vec8<DT>*>(at_global<T>(a.v) + row * a.d + 8 * lane), v);
 }
 
 int check(int64_t tokens, int32_t heads, int32_t d, int64_t pages, int32_t page_size, int dtype, int format)
@@ -166,13 +189,13 @@ int check(int64_t tokens, int32_t heads, int32_t d, int64_t pages, int32_t page_
 
 int launched(hipError_t e) { return e == hipSuccess ? ADDRMS_OK : fail(ADDRMS_ERR_HIP, "the launch failed: %s", hipGetErrorString(e)); }
 
-CacheArgs args_of(const int64_t* slots, int64_t tokens, int32_t heads, int32_t d, int64_t pages, int32_t page_size, int32_t piece)
+CacheArgs args_of(const int64_t* slots, int64_t tokens, int32_t heads, int32_t d, int64_t pages, int32_t page_size)
 {
     CacheArgs a = {};
     a.slots = addr(slots);
     a.rows = tokens * heads, a.cache_slots = pages * page_size;
     a.heads = static_cast<uint32_t>(heads), a.d = static_cast<uint32_t>(d);
-    a.page_shift = static_cast<uint32_t>(log2_of(page_size)), a.lanes_log2 = static_cast<uint32_t>(log2_of(d / piece));
+    a.page_shift = static_cast<uint32_t>(log2_of(page_size)), a.lanes_log2 = static_cast<uint32_t>(log2_of(d / 8));
     return a;
 }
 unsigned grid_of(const CacheArgs& a)
@@ -195,7 +218,7 @@ int kvcache_write(const void* k, const int64_t* k_strides, const void* v, const 
         return fail(ADDRMS_ERR_INVALID_ARG, "no pointer may be NULL");
     if (!aligned_to(k, 2) || !aligned_to(v, 2) || !aligned_to(slots, 8) || !aligned_to(k_pages, 16) || !aligned_to(v_pages, 16))
         return fail(ADDRMS_ERR_MISALIGNED, "k and v must be aligned to their elements, slots to 8 bytes and pages to 16");
-    CacheArgs a = args_of(slots, tokens, heads, d, pages, page_size, 8);
+    CacheArgs a = args_of(slots, tokens, heads, d, pages, page_size);
     a.k = addr(k), a.v = addr(v), a.k_pages = addr(k_pages), a.v_pages = addr(v_pages), a.k_scale = addr(k_scale), a.v_scale = addr(v_scale);
     uint64_t bits = a.k | a.v;
     for (int i = 0; i < 2; ++i) {
@@ -205,10 +228,12 @@ int kvcache_write(const void* k, const int64_t* k_strides, const void* v, const 
     const bool wide = bits % 16 == 0;        // else element by element
     const dim3 grid(grid_of(a));
     const hipStream_t s = static_cast<hipStream_t>(stream);
-#define GO(DT, F)                                                               \
-    do {                                                                        \
-        if (wide) write_kernel<DT, F, true><<<grid, kThreads, 0, s>>>(a);       \
-        else write_kernel<DT, F, false><<<grid, kThreads, 0, s>>>(a);           \
+    const bool past = a.rows * d * 4 >= kPastBytes;
+#define GO(DT, F)                                                                     \
+    do {                                                                              \
+        if (wide && past) write_kernel<DT, F, true, true><<<grid, kThreads, 0, s>>>(a);   \
+        else if (wide) write_kernel<DT, F, true, false><<<grid, kThreads, 0, s>>>(a);     \
+        else write_kernel<DT, F, false, false><<<grid, kThreads, 0, s>>>(a);              \
     } while (0)
     if (dtype == ADDRMS_BF16 && format == KVCACHE_E4M3) GO(DT_BF16, KVCACHE_E4M3);
     else if (dtype == ADDRMS_BF16) GO(DT_BF16, KVCACHE_SAME);
@@ -227,14 +252,21 @@ int kvcache_read(const void* k_pages, const void* v_pages, const uint8_t* k_scal
         return fail(ADDRMS_ERR_INVALID_ARG, "no pointer may be NULL");
     if (!aligned_to(k_out, 16) || !aligned_to(v_out, 16) || !aligned_to(slots, 8) || !aligned_to(k_pages, 16) || !aligned_to(v_pages, 16))
         return fail(ADDRMS_ERR_MISALIGNED, "pages and outputs must be 16-byte aligned and slots 8-byte");
-    CacheArgs a = args_of(slots, tokens, heads, d, pages, page_size, 16);
+    CacheArgs a = args_of(slots, tokens, heads, d, pages, page_size);
     a.k = addr(k_out), a.v = addr(v_out), a.k_pages = addr(k_pages), a.v_pages = addr(v_pages), a.k_scale = addr(k_scale), a.v_scale = addr(v_scale);
     const dim3 grid(grid_of(a));
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == ADDRMS_BF16 && format == KVCACHE_E4M3) read_kernel<DT_BF16, KVCACHE_E4M3><<<grid, kThreads, 0, s>>>(a);
-    else if (dtype == ADDRMS_BF16) read_kernel<DT_BF16, KVCACHE_SAME><<<grid, kThreads, 0, s>>>(a);
-    else if (format == KVCACHE_E4M3) read_kernel<DT_FP16, KVCACHE_E4M3><<<grid, kThreads, 0, s>>>(a);
-    else read_kernel<DT_FP16, KVCACHE_SAME><<<grid, kThreads, 0, s>>>(a);
+    const bool past = a.rows * d * 4 >= kPastBytes;
+#define GO(DT, F)                                                             \
+    do {                                                                      \
+        if (past) read_kernel<DT, F, true><<<grid, kThreads, 0, s>>>(a);          \
+        else read_kernel<DT, F, false><<<grid, kThreads, 0, s>>>(a);              \
+    } while (0)
+    if (dtype == ADDRMS_BF16 && format == KVCACHE_E4M3) GO(DT_BF16, KVCACHE_E4M3);
+    else if (dtype == ADDRMS_BF16) GO(DT_BF16, KVCACHE_SAME);
+    else if (format == KVCACHE_E4M3) GO(DT_FP16, KVCACHE_E4M3);
+    else GO(DT_FP16, KVCACHE_SAME);
+#undef GO
     return launched(hipGetLastError());
 }
 
