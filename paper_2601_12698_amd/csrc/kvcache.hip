@@ -16,11 +16,12 @@ using namespace serving;
 namespace {
 
 constexpr int kThreads = 256;
+constexpr uint32_t kBlock = 8;               // tokens of a head that are written side by side (16384 x 8 x 128: 21.4 us token by token, 19.8 with 8 or 16)
 constexpr int64_t kPastBytes = 4 << 20;      // of keys and values in 16 bits: the L2 of one XCD
 
 struct CacheArgs {
     addr_t k, v, slots, k_pages, v_pages, k_scale, v_scale;
-    int64_t rows, cache_slots;
+    int64_t tokens, rows, cache_slots;
     int64_t ks[2], vs[2];                    // strides of k and v: token, head
     uint32_t heads, d, lanes_log2, page_shift;
 };
@@ -96,10 +97,11 @@ __global__ __launch_bounds__(kThreads) void write_kernel(const CacheArgs a)
 {
     typedef typename elem<DT>::type T;
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
-    if (row >= a.rows) return;                                       // all lanes of a row together
-    const int64_t t = static_cast<int64_t>(static_cast<uint32_t>(row) / a.heads);
-    const uint32_t h = static_cast<uint32_t>(row - t * a.heads);
+    // eight tokens of one head, then of the next: their codes and scale bytes lie side by side
+    const uint32_t at = blockIdx.x * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2), block = at / (kBlock * a.heads), in_block = at - block * (kBlock * a.heads);
+    const uint32_t h = in_block / kBlock;
+    const int64_t t = static_cast<int64_t>(block) * kBlock + in_block % kBlock;
+    if (t >= a.tokens) return;                                       // all lanes of a row together
     const bool in = 8 * lane < a.d;
     const int64_t slot = at_global<const int64_t>(a.slots)[t];
     const vec8<DT> k = load8<DT, WIDE>(at_global<const T>(a.k) + t * a.ks[0] + h * a.ks[1] + 8 * lane, in);
@@ -182,7 +184,7 @@ int check(int64_t tokens, int32_t heads, int32_t d, int64_t pages, int32_t page_
     if (!power_of_two(page_size) || page_size > 65536) return fail(ADDRMS_ERR_INVALID_ARG, "page_size must be a power of two up to 65536 (got %d)", page_size);
     if (d % 16 != 0 || d > KVCACHE_MAX_HEAD)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "d=%d is not a multiple of 16 up to %d", d, KVCACHE_MAX_HEAD);
-    if (heads > 65536 || pages >= (1ll << 31) || tokens >= (1ll << 31) / heads)
+    if (heads > 65536 || pages >= (1ll << 31) || tokens >= (1ll << 31) / heads - kBlock)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld tokens of %d heads or %lld pages are beyond the limits", (long long)tokens, heads, (long long)pages);
     return ADDRMS_OK;
 }
@@ -193,15 +195,15 @@ CacheArgs args_of(const int64_t* slots, int64_t tokens, int32_t heads, int32_t d
 {
     CacheArgs a = {};
     a.slots = addr(slots);
-    a.rows = tokens * heads, a.cache_slots = pages * page_size;
+    a.tokens = tokens, a.rows = tokens * heads, a.cache_slots = pages * page_size;
     a.heads = static_cast<uint32_t>(heads), a.d = static_cast<uint32_t>(d);
     a.page_shift = static_cast<uint32_t>(log2_of(page_size)), a.lanes_log2 = static_cast<uint32_t>(log2_of(d / 8));
     return a;
 }
-unsigned grid_of(const CacheArgs& a)
+unsigned grid_of(const CacheArgs& a, int64_t tokens)
 {
     const int64_t per = kThreads >> a.lanes_log2;
-    return static_cast<unsigned>((a.rows + per - 1) / per);
+    return static_cast<unsigned>((tokens * a.heads + per - 1) / per);
 }
 
 }  // namespace
@@ -226,7 +228,7 @@ int kvcache_write(const void* k, const int64_t* k_strides, const void* v, const 
         bits |= static_cast<uint64_t>(a.ks[i] | a.vs[i]) * 2;
     }
     const bool wide = bits % 16 == 0;        // else element by element
-    const dim3 grid(grid_of(a));
+    const dim3 grid(grid_of(a, (tokens + kBlock - 1) / kBlock * kBlock));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool past = a.rows * d * 4 >= kPastBytes;
 #define GO(DT, F)                                                                     \
@@ -254,7 +256,7 @@ int kvcache_read(const void* k_pages, const void* v_pages, const uint8_t* k_scal
         return fail(ADDRMS_ERR_MISALIGNED, "pages and outputs must be 16-byte aligned and slots 8-byte");
     CacheArgs a = args_of(slots, tokens, heads, d, pages, page_size);
     a.k = addr(k_out), a.v = addr(v_out), a.k_pages = addr(k_pages), a.v_pages = addr(v_pages), a.k_scale = addr(k_scale), a.v_scale = addr(v_scale);
-    const dim3 grid(grid_of(a));
+    const dim3 grid(grid_of(a, tokens));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool past = a.rows * d * 4 >= kPastBytes;
 #define GO(DT, F)                                                             \
