@@ -20,10 +20,11 @@ struct AttnArgs {
     float c;                                          // scale * log2(e): weights are powers of 2
 };
 
-// Forms of a workgroup: 16 rows whose waves take keys in turn; 64, 128 or 256 rows that share their keys (256: heads of 65 to 128).
-enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2, MANY_256 = 3 };
+// Forms of a workgroup: 16 rows whose four (FEW_8: eight) waves take keys in turn; 64, 128 or 256 rows that share their keys (256:
+// heads of 65 to 128).
+enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2, MANY_256 = 3, FEW_8 = 4 };
 constexpr int kJoinThreads = 256;
-constexpr int kFormRows[] = {16, 64, 128, 256};
+constexpr int kFormRows[] = {16, 64, 128, 256, 16};
 constexpr int kChunkStep = 128;                       // splits begin at multiples of this many keys: every tile is aligned
 constexpr int kFinishSplits = 64;                     // of a prefix that is joined by the suffixes' workgroups: a part a lane
 constexpr int kMaxSplits = 256;                       // of a prefix, and of a suffix

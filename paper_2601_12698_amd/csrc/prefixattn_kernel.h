@@ -657,9 +657,10 @@ struct Many {
 // Workgroups of the prefix first, then those of the suffixes.  Workgroups go round the 8 XCDs; the row tiles of one head and
 // key range stand 8 apart, so that they read it through the same L2 at the same time.
 // FORM: see prefixattn_args.h.
-template <int DP> constexpr int threads_of(int form) { return form == MANY_256 || (form == MANY_128 && DP > 128) ? 512 : 256; }
+template <int DP> constexpr int threads_of(int form) { return form == FEW_8 || form == MANY_256 || (form == MANY_128 && DP > 128) ? 512 : 256; }
 template <int DT, int FORMAT, int DP, int FORM, int WAVES> struct form;
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW, WAVES> { typedef Few<DT, FORMAT, DP, WAVES> type; };
+template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW_8, WAVES> { typedef Few<DT, FORMAT, DP, 8> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_64, WAVES> { typedef Many<DT, FORMAT, DP, 16, 4> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_128, WAVES> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4)> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8> type; };
@@ -688,7 +689,7 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW 
         s.end = min(s.first + a.prefix_chunk, a.prefix_len);
         s.part = split;
         s.last0 = kAll;
-        if constexpr (PREFIX == FEW) P().run(a, s, P::page_of(a, s, s.first + P::TILE * (threadIdx.x >> 6), threadIdx.x & 63), lds);
+        if constexpr (PREFIX == FEW || PREFIX == FEW_8) P().run(a, s, P::page_of(a, s, s.first + P::TILE * (threadIdx.x >> 6), threadIdx.x & 63), lds);
         else P().run(a, s, lds);
         return;
     }
@@ -706,7 +707,7 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW 
     s.part = a.prefix_splits + split;
     s.first = split * a.suffix_chunk;
     s.table = a.suffix_pages + 4 * static_cast<int64_t>(seq) * a.suffix_width;
-    if constexpr (SUFFIX == FEW) {
+    if constexpr (SUFFIX == FEW || SUFFIX == FEW_8) {
         if (a.inline_len) {
             s.table2 = s.table;
             s.table = a.prefix_pages;
