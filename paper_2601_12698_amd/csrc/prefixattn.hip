@@ -2,6 +2,8 @@
 // that joins the splits' results.
 #include <math.h>
 
+#include <algorithm>
+
 #include "prefixattn.h"
 #include "prefixattn_args.h"
 #include "serving_internal.h"
@@ -171,22 +173,23 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         p->suffix_blocks = static_cast<int64_t>(a.kv_heads) * s->batch;
         return p->suffix_blocks > kMaxBlocks ? fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)p->suffix_blocks) : ADDRMS_OK;
     }
-    if (a.prefix_len && a.pages) {
-        a.prefix_tiles = static_cast<int32_t>(tiles(all, p->prefix_form));
-        a.prefix_splits = splits_of(a.prefix_len, static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, wanted(p->prefix_form), &a.prefix_chunk);
-        p->prefix_blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
-    } else {
-        p->prefix_form = p->suffix_form;
+    const bool prefix = a.prefix_len && a.pages, suffix = width && a.pages;
+    if (!prefix) p->prefix_form = p->suffix_form;
+    a.prefix_tiles = static_cast<int32_t>(tiles(all, p->prefix_form));
+    a.suffix_tiles = static_cast<int32_t>(tiles(own, p->suffix_form));
+    const int64_t prefix_units = static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, suffix_units = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads * s->batch;
+    const int64_t slots = wanted(p->prefix_form);
+    auto split_prefix = [&](int64_t n) { a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, n, &a.prefix_chunk) : 0; };
+    split_prefix(slots);
+    p->finish = suffix && suffix_units >= kFinishUnits && a.prefix_splits <= kFinishSplits;
+    if (suffix) {
+        a.suffix_splits = splits_of(width, suffix_units, p->finish ? 1 : wanted(p->suffix_form), &a.suffix_chunk);
+        p->suffix_blocks = suffix_units * a.suffix_splits;
+        // one launch for both: the prefix leaves the suffixes their places, up to half of all
+        if (!p->finish && prefix) split_prefix(std::max(slots / 2, slots - p->suffix_blocks));
     }
-    int64_t parts = a.prefix_splits;
-    if (width && a.pages) {
-        a.suffix_tiles = static_cast<int32_t>(tiles(own, p->suffix_form));
-        const int64_t units = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads * s->batch;
-        p->finish = units >= kFinishUnits && a.prefix_splits <= kFinishSplits;
-        a.suffix_splits = splits_of(width, units, p->finish ? 1 : wanted(p->suffix_form), &a.suffix_chunk);
-        p->suffix_blocks = units * a.suffix_splits;
-        if (!p->finish) parts += a.suffix_splits;
-    }
+    p->prefix_blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
+    const int64_t parts = a.prefix_splits + (p->finish ? 0 : a.suffix_splits);
     if (p->prefix_blocks + p->suffix_blocks > kMaxBlocks)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)(p->prefix_blocks + p->suffix_blocks));
     p->bytes = parts * p->rows * (4ll * a.d + 8);
