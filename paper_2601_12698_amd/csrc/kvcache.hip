@@ -93,7 +93,7 @@ __device__ __forceinline__ void quantise(vec8<DT> raw, bool in, uint32_t lanes, 
 }
 
 template <int DT, int FORMAT, bool WIDE, bool PAST>
-__global__ __launch_bounds__(kThreads) void write_kernel(const CacheArgs a)
+__global__ __launch_bounds__(kThreads) void write_kernel(CacheArgs a)
 {
     typedef typename elem<DT>::type T;
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
@@ -154,7 +154,7 @@ struct Piece {
 };
 
 template <int DT, int FORMAT, bool PAST>
-__global__ __launch_bounds__(kThreads) void read_kernel(const CacheArgs a)
+__global__ __launch_bounds__(kThreads) void read_kernel(CacheArgs a)
 {
     const uint32_t lanes = 1u << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
@@ -231,18 +231,10 @@ int kvcache_write(const void* k, const int64_t* k_strides, const void* v, const 
     const dim3 grid(grid_of(a, (tokens + kBlock - 1) / kBlock * kBlock));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool past = a.rows * d * 4 >= kPastBytes;
-#define GO(DT, F)                                                                     \
-    do {                                                                              \
-        if (wide && past) write_kernel<DT, F, true, true><<<grid, kThreads, 0, s>>>(a);   \
-        else if (wide) write_kernel<DT, F, true, false><<<grid, kThreads, 0, s>>>(a);     \
-        else write_kernel<DT, F, false, false><<<grid, kThreads, 0, s>>>(a);              \
-    } while (0)
-    if (dtype == ADDRMS_BF16 && format == KVCACHE_E4M3) GO(DT_BF16, KVCACHE_E4M3);
-    else if (dtype == ADDRMS_BF16) GO(DT_BF16, KVCACHE_SAME);
-    else if (format == KVCACHE_E4M3) GO(DT_FP16, KVCACHE_E4M3);
-    else GO(DT_FP16, KVCACHE_SAME);
+#define GO(DT, F) launch_kernel(!wide ? write_kernel<DT, F, false, false> : past ? write_kernel<DT, F, true, true> : write_kernel<DT, F, true, false>, grid, kThreads, s, a)
+    if (dtype == ADDRMS_BF16) return launched(format == KVCACHE_E4M3 ? GO(DT_BF16, KVCACHE_E4M3) : GO(DT_BF16, KVCACHE_SAME));
+    return launched(format == KVCACHE_E4M3 ? GO(DT_FP16, KVCACHE_E4M3) : GO(DT_FP16, KVCACHE_SAME));
 #undef GO
-    return launched(hipGetLastError());
 }
 
 int kvcache_read(const void* k_pages, const void* v_pages, const uint8_t* k_scale, const uint8_t* v_scale, const int64_t* slots, void* k_out, void* v_out,
@@ -259,17 +251,10 @@ int kvcache_read(const void* k_pages, const void* v_pages, const uint8_t* k_scal
     const dim3 grid(grid_of(a, tokens));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool past = a.rows * d * 4 >= kPastBytes;
-#define GO(DT, F)                                                             \
-    do {                                                                      \
-        if (past) read_kernel<DT, F, true><<<grid, kThreads, 0, s>>>(a);          \
-        else read_kernel<DT, F, false><<<grid, kThreads, 0, s>>>(a);              \
-    } while (0)
-    if (dtype == ADDRMS_BF16 && format == KVCACHE_E4M3) GO(DT_BF16, KVCACHE_E4M3);
-    else if (dtype == ADDRMS_BF16) GO(DT_BF16, KVCACHE_SAME);
-    else if (format == KVCACHE_E4M3) GO(DT_FP16, KVCACHE_E4M3);
-    else GO(DT_FP16, KVCACHE_SAME);
+#define GO(DT, F) launch_kernel(past ? read_kernel<DT, F, true> : read_kernel<DT, F, false>, grid, kThreads, s, a)
+    if (dtype == ADDRMS_BF16) return launched(format == KVCACHE_E4M3 ? GO(DT_BF16, KVCACHE_E4M3) : GO(DT_BF16, KVCACHE_SAME));
+    return launched(format == KVCACHE_E4M3 ? GO(DT_FP16, KVCACHE_E4M3) : GO(DT_FP16, KVCACHE_SAME));
 #undef GO
-    return launched(hipGetLastError());
 }
 
 int64_t kvcache_algorithmic_bytes(int64_t tokens, int32_t heads, int32_t d, int dtype, int format)

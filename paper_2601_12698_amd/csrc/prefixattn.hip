@@ -18,7 +18,7 @@ namespace {
 // are under way while their weights are found.  One wave where there are rows enough to fill the chip (no barrier, four rows a
 // workgroup), four where there are few rows, which then have many parts.
 template <int DT, int WAVES>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttnArgs a)
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a)
 {
     typedef typename elem<DT>::type T;
     typedef T T4 __attribute__((ext_vector_type(4)));
@@ -257,9 +257,9 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
     if (p.prefix_blocks + p.suffix_blocks) SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.prefix_blocks + p.suffix_blocks), s));
     const bool many = p.rows >= kJoinRows;
     const unsigned groups = static_cast<unsigned>(many ? (p.rows + 3) / 4 : p.rows);
-    if (shape->dtype == ADDRMS_FP16) many ? join_kernel<DT_FP16, 1><<<groups, kJoinThreads, 0, s>>>(a) : join_kernel<DT_FP16, 4><<<groups, kJoinThreads, 0, s>>>(a);
-    else many ? join_kernel<DT_BF16, 1><<<groups, kJoinThreads, 0, s>>>(a) : join_kernel<DT_BF16, 4><<<groups, kJoinThreads, 0, s>>>(a);
-    SERVING_HIP_TRY(hipGetLastError());
+    SERVING_HIP_TRY(launch_kernel(shape->dtype == ADDRMS_FP16 ? (many ? join_kernel<DT_FP16, 1> : join_kernel<DT_FP16, 4>)
+                                                              : (many ? join_kernel<DT_BF16, 1> : join_kernel<DT_BF16, 4>),
+                                  dim3(groups), dim3(kJoinThreads), s, a));
     return ADDRMS_OK;
 }
 

@@ -43,6 +43,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLazy = 8.0f;                                   // a maximum may lag behind by this power of 2
+constexpr float kMost = 0x1.fffffep127f;
 // fp16 weights are 2^7 times larger (at most 2^15), so that they are normal numbers down to 2^-21 of the largest.
 template <int DT> constexpr float kLift = DT == DT_FP16 ? 7.0f : 0.0f;
 constexpr uint64_t full_of(int bits) { return bits == 64 ? ~0ull : (1ull << bits) - 1; }
@@ -90,7 +91,7 @@ struct Share {
     addr_t table, table2;
     int32_t turn, head, token0, row0, rows, first, end, part, last0;
 };
-constexpr int32_t kAll = 1 << 30;
+constexpr int32_t kAll = 0x7fffffff;
 __device__ __forceinline__ int32_t page_at(const AttnArgs& a, const Share& s, int32_t key)
 {
     const bool second = key >= s.turn;
@@ -234,7 +235,7 @@ struct Few {
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = f32x4{0, 0, 0, 0};
         float m = kNone, l = 0.0f;
-        const float lag = kLazy / a.c;
+        const float lag = fminf(kLazy / a.c, kMost);
         char* mine = lds + wave * WAVE_LDS;
         // where this lane's 8 bytes of a transposing read begin: key 4 g + (lane % 16) / 4 of 16, elements 4 (lane % 4) of 16
         const char* from = mine + (4 * g + ((lane & 15) >> 2)) * VROW + 8 * (lane & 3);
@@ -508,7 +509,7 @@ struct Many {
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = A{};
         float m = kNone, l = 0.0f;
-        const float lag = kLazy / a.c;
+        const float lag = fminf(kLazy / a.c, kMost);
 
         const auto attend = [&](const char* buf, int32_t key0) {
             const char* kt = buf + r * KROW + 16 * g;
@@ -666,7 +667,7 @@ template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MAN
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8> type; };
 
 template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX>
-__global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW ? 1 : 2)) void attn_kernel(const AttnArgs a)
+__global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW ? 1 : 2)) void attn_kernel(AttnArgs a)
 {
     constexpr int WAVES = threads_of<DP>(PREFIX) / 64;          // few rows use all of them, whatever the prefix's form
     typedef typename form<DT, FORMAT, DP, PREFIX, WAVES>::type P;

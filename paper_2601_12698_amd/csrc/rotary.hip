@@ -58,7 +58,7 @@ template <typename T, int V> struct piece { typedef T type __attribute__((ext_ve
 // 2 j on (V = 1: one pair, both elements).  blockDim.x = pieces of a head (pairs, or V elements that are copied), blockDim.y = heads
 // side by side.  PAST: outputs are written past the caches.
 template <int DT, int V, bool INTER, bool PAST>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a)
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
 {
     typedef typename elem<DT>::type T;
     typedef typename piece<T, V>::type P;
@@ -145,9 +145,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a)
 template <int DT, int V>
 hipError_t launch(const RotaryArgs& a, bool inter, bool past, dim3 grid, dim3 block, hipStream_t s)
 {
-    if (inter) past ? rotary_kernel<DT, V, true, true><<<grid, block, 0, s>>>(a) : rotary_kernel<DT, V, true, false><<<grid, block, 0, s>>>(a);
-    else past ? rotary_kernel<DT, V, false, true><<<grid, block, 0, s>>>(a) : rotary_kernel<DT, V, false, false><<<grid, block, 0, s>>>(a);
-    return hipGetLastError();
+    if (inter) return launch_kernel(past ? rotary_kernel<DT, V, true, true> : rotary_kernel<DT, V, true, false>, grid, block, s, a);
+    return launch_kernel(past ? rotary_kernel<DT, V, false, true> : rotary_kernel<DT, V, false, false>, grid, block, s, a);
 }
 
 // True if the bytes that [tokens, heads, d] with these strides spans hold two elements at one place.

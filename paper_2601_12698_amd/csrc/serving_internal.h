@@ -71,6 +71,14 @@ inline int log2_of(int64_t n)
     return s;
 }
 
+// A launch whose status is its own: an error that other code of the process left behind is not taken for it.
+template <typename Args>
+hipError_t launch_kernel(void (*kernel)(Args), dim3 grid, dim3 block, hipStream_t stream, const Args& args)
+{
+    void* p[] = {const_cast<Args*>(&args)};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, p, 0, stream);
+}
+
 #define SERVING_HIP_TRY(expr)                                                                                     \
     do {                                                                                                          \
         const hipError_t e_ = (expr);                                                                             \

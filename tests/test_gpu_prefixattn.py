@@ -175,6 +175,13 @@ def test_large_scores_and_a_late_maximum(quantised, batch, prefix):
     check(c, dtype, got)
 
 
+@pytest.mark.parametrize("scale", [1e-39, 1e-37])
+def test_a_scale_that_makes_all_scores_alike(scale):
+    c, dtype = build((20, 1, 4, 1, 64, 800, [5] * 20, 1, 16, "bf16", True), seed=11)
+    c["scale"] = scale
+    check(c, dtype, call(c, dtype))
+
+
 @pytest.mark.parametrize("prefix", [100, 800])
 def test_nan_in_a_seen_key_reaches_its_row_alone(prefix):
     c, dtype = build((20, 1, 4, 2, 64, prefix, [5] * 20, 1, 16, "bf16", False), seed=7)
