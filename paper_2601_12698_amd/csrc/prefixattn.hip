@@ -147,7 +147,8 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     a.batch = s->batch, a.q_len = s->q_len, a.q_heads = s->q_heads, a.kv_heads = s->kv_heads, a.group = s->q_heads / s->kv_heads, a.d = s->d;
     a.page_shift = log2_of(s->page_size), a.pages = static_cast<int32_t>(s->pages);
     a.prefix_len = static_cast<int32_t>(s->prefix_len), a.suffix_width = static_cast<int32_t>(s->suffix_width);
-    a.page_rows = static_cast<uint64_t>(page_rows), a.page_bytes = static_cast<uint64_t>(page_rows * row_bytes);
+    a.page_rows = static_cast<uint32_t>(page_rows), a.page_bytes = static_cast<uint32_t>(page_rows * row_bytes);
+    a.head_bytes = static_cast<uint32_t>(s->page_size * row_bytes);
     p->dp = s->d <= 64 ? 64 : s->d <= 128 ? 128 : 256;
     if (s->batch == 0 || s->q_len == 0) return ADDRMS_OK;
     const int64_t tokens = static_cast<int64_t>(s->batch) * s->q_len;
@@ -185,8 +186,14 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     if (suffix) {
         a.suffix_splits = splits_of(width, suffix_units, p->finish ? 1 : wanted(p->suffix_form), &a.suffix_chunk);
         p->suffix_blocks = suffix_units * a.suffix_splits;
-        // one launch for both: the prefix leaves the suffixes their places, up to half of all
-        if (!p->finish && prefix) split_prefix(std::max(slots / 2, slots - p->suffix_blocks));
+        // One launch for both: the prefix leaves the suffixes their places, up to half of all, unless its pieces grow by more keys than
+        // a suffix's piece has, which then runs behind them (16 x 4 queries over 4001 fp16 keys of 256 and suffixes of 300: behind 53.6
+        // us, beside 43.4; 8 x 40 heads over 131072 e4m3 keys and suffixes of 500: behind 75.2, beside 87.5).
+        if (!p->finish && prefix) {
+            const int32_t splits = a.prefix_splits, chunk = a.prefix_chunk;
+            split_prefix(std::max(slots / 2, slots - p->suffix_blocks));
+            if (a.prefix_chunk - chunk > std::min<int64_t>(width, a.suffix_chunk)) a.prefix_splits = splits, a.prefix_chunk = chunk;
+        }
     }
     p->prefix_blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
     const int64_t parts = a.prefix_splits + (p->finish ? 0 : a.suffix_splits);

@@ -13,7 +13,7 @@ struct AttnArgs {
     int32_t batch, q_len, q_heads, kv_heads, group, d, page_shift, pages;
     int32_t prefix_len, prefix_splits, prefix_chunk, prefix_tiles, prefix_blocks;
     int32_t suffix_width, suffix_splits, suffix_chunk, suffix_tiles;
-    uint64_t page_bytes, page_rows;                   // of a page: all its heads
+    uint32_t page_bytes, page_rows, head_bytes;       // of a page: all its heads, and one
     int32_t inline_len;                               // keys of a short prefix that each suffix's workgroup sees itself, before its own
     int32_t finish;                                   // the suffixes' workgroups join the prefix's parts to their own, and write the output
     int32_t q_wide;                                   // queries can be read 16 bytes at a time

@@ -123,8 +123,10 @@ struct Place {
 };
 __device__ __forceinline__ Place place_of(const AttnArgs& a, int32_t head, int32_t page, int32_t key, int32_t row_bytes)
 {
-    const uint32_t in = (static_cast<uint32_t>(head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));       // below 2^32 / row_bytes
-    return Place{static_cast<uint64_t>(page) * a.page_bytes + in * static_cast<uint32_t>(row_bytes), static_cast<uint64_t>(page) * a.page_rows + in};
+    // 32-bit factors, and one of 24 bits (an offset in a page times a row's bytes): a 64-bit product is four slow instructions
+    const uint32_t in = static_cast<uint32_t>(key) & ((1u << a.page_shift) - 1);
+    return Place{static_cast<uint64_t>(static_cast<uint32_t>(page)) * a.page_bytes + (static_cast<uint32_t>(head) * a.head_bytes + __umul24(in, row_bytes)),
+                 static_cast<uint64_t>(static_cast<uint32_t>(page)) * a.page_rows + ((static_cast<uint32_t>(head) << a.page_shift) + in)};
 }
 __device__ __forceinline__ bool in_cache(const AttnArgs& a, int32_t page) { return static_cast<uint32_t>(page) < static_cast<uint32_t>(a.pages); }
 
@@ -405,17 +407,18 @@ struct Few {
     }
 };
 
-template <int DT, int FORMAT, int DP, int RW, int WAVES>
+template <int DT, int FORMAT, int DP, int RW, int WAVES, int KS = 1>
 struct Many {
     typedef mat<DT> M;
     typedef typename M::T T;
     typedef typename M::T8 T8;
     static constexpr bool CODES = FORMAT == KVCACHE_E4M3, WIDE = RW == 32;
-    static constexpr int ES = CODES ? 1 : 2, THREADS = 64 * WAVES, ROWS = RW * WAVES;
+    static constexpr int ES = CODES ? 1 : 2, THREADS = 64 * WAVES, GROUPS = WAVES / KS, ROWS = RW * GROUPS;
     static constexpr int TILE = DP > 128 && WAVES == 4 ? 32 : 64;   // keys at a time: two workgroups' tiles, or one of eight waves, fit a CU
+    static constexpr int KEYS = TILE / KS;                      // of a wave
     typedef typename acc<RW>::type A;                           // of a lane: WIDE 16 of 32 keys (or elements) by rows, else 4 of 16
     static constexpr int AN = WIDE ? 16 : 4;
-    static constexpr int NS = TILE / RW;                        // pieces of S
+    static constexpr int NS = KEYS / RW;                        // pieces of S
     static constexpr int KC = WIDE ? 16 : 32;                   // elements, or keys, that one matrix instruction sums over
     static constexpr int NC = DP / KC;
     static constexpr int NT = DP / RW;                          // pieces of O
@@ -502,8 +505,9 @@ struct Many {
     {
         // lane = row, and one of 2 (WIDE) or 4 groups of keys or elements
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
-        const Row row = row_of(a, s, RW * wave + r);
-        const bool busy = RW * wave < s.rows;                   // waves without rows only help to stage
+        const int group = wave % GROUPS, part = wave / GROUPS * KEYS;      // its rows, and its keys of a tile
+        const Row row = row_of(a, s, RW * group + r);
+        const bool busy = RW * group < s.rows;                   // waves without rows only help to stage
         T8 q[NC];
         A o[NT];
 #pragma unroll
@@ -512,7 +516,7 @@ struct Many {
         const float lag = fminf(kLazy / a.c, kMost);
 
         const auto attend = [&](const char* buf, int32_t key0) {
-            const char* kt = buf + r * KROW + 16 * g;
+            const char* kt = buf + (part + r) * KROW + 16 * g;
             A z[NS];
 #pragma unroll
             for (int t = 0; t < NS; ++t) {
@@ -523,8 +527,8 @@ struct Many {
             const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane % TILE] != 0) & full_of(TILE);
             if (there != full_of(TILE) || key0 + TILE - 1 > s.last0) {
                 // this lane's keys, shifted so that each is a fixed bit (a mask made for every score would be held in registers)
-                const uint64_t mine = there >> (4 * g);
-                const int32_t last = row.last - key0 - 4 * g;
+                const uint64_t mine = there >> (part + 4 * g);
+                const int32_t last = row.last - key0 - part - 4 * g;
 #pragma unroll
                 for (int t = 0; t < NS; ++t)
 #pragma unroll
@@ -550,9 +554,9 @@ struct Many {
             }
             const float base = m == kNone ? 0.0f : m * a.c - kLift<DT>;
             // where this lane's 8 bytes of a transposing read begin: of 4 keys, its (lane % 16) / 4 th, elements 4 (lane % 4) of 16
-            const char* vt = buf + TILE * KROW + (4 * g + ((lane & 15) >> 2)) * VROW + (WIDE ? 32 * ((lane >> 4) & 1) : 0) + 8 * (lane & 3);
+            const char* vt = buf + TILE * KROW + (part + 4 * g + ((lane & 15) >> 2)) * VROW + (WIDE ? 32 * ((lane >> 4) & 1) : 0) + 8 * (lane & 3);
 #pragma unroll
-            for (int u = 0; u < TILE / KC; ++u) {
+            for (int u = 0; u < KEYS / KC; ++u) {
                 T8 p;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -578,17 +582,26 @@ struct Many {
             pages_of(a, s, s.first + TILE, page);
 #pragma unroll
             for (int c = 0; c < NC; ++c) q[c] = query_piece<DT>(a, row, KC * c + 8 * g);
-            if (s.first + TILE < s.end) odd.load(a, s, s.first + TILE, page);
-            pages_of(a, s, s.first + 2 * TILE, page);
+            {
+                int32_t now[NP];
+#pragma unroll
+                for (int i = 0; i < NP; ++i) now[i] = page[i];
+                pages_of(a, s, s.first + 2 * TILE, page);
+                odd.load(a, s, s.first + TILE, now);
+            }
             even.clear(a);
             even.stage(lds);
             __syncthreads();
             // one turn: `key0`'s tile is in `buf`, the next one arrives in `next`, the one after is asked for into `after`
             const auto turn = [&](int32_t key0, char* buf, char* other, Staged& next, Staged& after) {
-                if (key0 + 2 * TILE < s.end) {
-                    after.load(a, s, key0 + 2 * TILE, page);
-                    pages_of(a, s, key0 + 3 * TILE, page);
-                }
+                // Page numbers are asked for before the pieces, and both in every turn, also for tiles that are beyond the end (whose keys
+                // then are not there): loads come back in their order and are waited for by their number, so that a page number behind
+                // its turn's pieces, or loads in a branch, would make every wait one for the newest.
+                int32_t now[NP];
+#pragma unroll
+                for (int i = 0; i < NP; ++i) now[i] = page[i];
+                pages_of(a, s, key0 + 3 * TILE, page);
+                after.load(a, s, key0 + 2 * TILE, now);
                 if (busy) attend(buf, key0);
                 if (key0 + TILE < s.end) {
                     next.clear(a);
@@ -596,10 +609,33 @@ struct Many {
                 }
                 __syncthreads();
             };
-            for (int32_t key0 = s.first; key0 < s.end; key0 += 2 * TILE) {
+            int32_t key0 = s.first;
+            for (; key0 + TILE < s.end; key0 += 2 * TILE) {
                 turn(key0, lds, lds + BUF, odd, even);
-                if (key0 + TILE >= s.end) break;
                 turn(key0 + TILE, lds + BUF, lds, even, odd);
+            }
+            if (key0 < s.end) turn(key0, lds, lds + BUF, odd, even);
+        }
+        if constexpr (KS == 2) {
+            // what the waves of a tile's other half found, register by register
+            constexpr int N = NT * AN;
+            static_assert(GROUPS * (N + 2) * 64 * 4 <= LDS, "the other half's results do not fit");
+            float* at = reinterpret_cast<float*>(lds) + group * (N + 2) * 64 + lane;
+            if (part && busy) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) at[64 * i] = o[i / AN][i % AN];
+                at[64 * N] = m;
+                at[64 * (N + 1)] = l;
+            }
+            __syncthreads();
+            if (part) return;
+            if (busy) {
+                const float other = at[64 * N], most = larger(m, other);
+                const float mine = m == kNone ? 1.0f : __builtin_amdgcn_exp2f((m - most) * a.c), its = other == kNone ? 1.0f : __builtin_amdgcn_exp2f((other - most) * a.c);
+#pragma unroll
+                for (int i = 0; i < N; ++i) o[i / AN][i % AN] = o[i / AN][i % AN] * mine + at[64 * i] * its;
+                l = l * mine + at[64 * (N + 1)] * its;
+                m = most;
             }
         }
         if (!busy) return;
@@ -662,7 +698,7 @@ template <int DP> constexpr int threads_of(int form) { return form == FEW_8 || f
 template <int DT, int FORMAT, int DP, int FORM, int WAVES> struct form;
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW, WAVES> { typedef Few<DT, FORMAT, DP, WAVES> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW_8, WAVES> { typedef Few<DT, FORMAT, DP, 8> type; };
-template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_64, WAVES> { typedef Many<DT, FORMAT, DP, 16, 4> type; };
+template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_64, WAVES> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), 4, (DP > 128 ? 1 : 2)> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_128, WAVES> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4)> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8> type; };
 
