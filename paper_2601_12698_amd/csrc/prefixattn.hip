@@ -186,13 +186,15 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     if (suffix) {
         a.suffix_splits = splits_of(width, suffix_units, p->finish ? 1 : wanted(p->suffix_form), &a.suffix_chunk);
         p->suffix_blocks = suffix_units * a.suffix_splits;
-        // One launch for both: the prefix leaves the suffixes their places, up to half of all, unless its pieces grow by more keys than
-        // a suffix's piece has, which then runs behind them (16 x 4 queries over 4001 fp16 keys of 256 and suffixes of 300: behind 53.6
-        // us, beside 43.4; 8 x 40 heads over 131072 e4m3 keys and suffixes of 500: behind 75.2, beside 87.5).
+        // One launch for both: the prefix leaves the suffixes their places, up to half of all.  Where a workgroup's own pace is the bound
+        // (not with few rows, where memory is), only if its pieces grow by no more keys than a suffix's piece has, which else runs behind
+        // them: 16 x 4 queries over 4001 fp16 keys of 256 and suffixes of 300 take 53.6 us with them behind, 43.4 beside; 8 x 40 heads
+        // over 131072 e4m3 keys and suffixes of 500 75.2 behind, 87.5 beside; with few rows, 4 x 32 heads over 131072 bf16 keys and
+        // suffixes of 2000, 106.0 behind, 103.2 beside.
         if (!p->finish && prefix) {
             const int32_t splits = a.prefix_splits, chunk = a.prefix_chunk;
             split_prefix(std::max(slots / 2, slots - p->suffix_blocks));
-            if (a.prefix_chunk - chunk > std::min<int64_t>(width, a.suffix_chunk)) a.prefix_splits = splits, a.prefix_chunk = chunk;
+            if (p->prefix_form != FEW && a.prefix_chunk - chunk > std::min<int64_t>(width, a.suffix_chunk)) a.prefix_splits = splits, a.prefix_chunk = chunk;
         }
     }
     p->prefix_blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
