@@ -163,10 +163,13 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
     // a CU holds one workgroup of eight waves, two of four that share keys, three of those with few rows
     auto wanted = [p](int form) { return form == FEW ? 768 : form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
+    // one workgroup a CU, or fewer: eight waves each (32 x 8 heads of e4m3 keys, 16 and then up to 1024: 15.0 us a call with four, 12.5
+    // with eight; 64 x 8: 17.6 with four, 21.8 with eight), unless their registers do not suffice (prefixattn_args.h)
+    const bool eight = few_8_fits(s->format, p->dp);
+    auto few = [eight](int64_t units) { return eight && units <= kFinishUnits ? FEW_8 : FEW; };
     if (a.pages && a.prefix_len && p->suffix_form == FEW && a.prefix_len <= kInlineKeys &&
         (static_cast<int64_t>(a.kv_heads) * s->batch >= kFinishUnits || a.prefix_len + width <= 2 * kInlineKeys)) {
-        // CUs to spare: eight waves a workgroup (two sequences over 301 keys: 8.7 us a call with four, 8.5 with eight)
-        p->prefix_form = p->suffix_form = static_cast<int64_t>(a.kv_heads) * s->batch < kFinishUnits ? FEW_8 : FEW;
+        p->prefix_form = p->suffix_form = few(static_cast<int64_t>(a.kv_heads) * s->batch);
         p->finish = true;
         a.inline_len = a.prefix_len;
         a.suffix_tiles = a.suffix_splits = 1;
@@ -183,6 +186,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     auto split_prefix = [&](int64_t n) { a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, n, &a.prefix_chunk) : 0; };
     split_prefix(slots);
     p->finish = suffix && suffix_units >= kFinishUnits && a.prefix_splits <= kFinishSplits;
+    if (p->finish && p->suffix_form == FEW) p->suffix_form = few(suffix_units);
     if (suffix) {
         a.suffix_splits = splits_of(width, suffix_units, p->finish ? 1 : wanted(p->suffix_form), &a.suffix_chunk);
         p->suffix_blocks = suffix_units * a.suffix_splits;
