@@ -99,15 +99,18 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a)
 }
 
 constexpr int64_t kMaxBlocks = 1 << 24;      // of 256 threads: a launch has fewer than 2^32
-constexpr int32_t kMinChunk = 256;
+// The shortest piece of keys; of a suffix as long as the prefix's, up to twice this.  128 beside 256, whole calls: 8 x 40 heads over
+// 2000 bf16 keys 12.8 and 14.2 us, 2 x 40 over 900 e4m3 10.8 and 11.2, 8 x 40 over 8191 the same; a long prefix with the suffixes in
+// pieces of 128 has too little room left: 4 x 32 heads over 131072 bf16 keys and suffixes of 2000 112 us, with pieces of 256 103.5.
+constexpr int32_t kMinChunk = 128;
 constexpr int64_t kInlineKeys = 512;         // up to here a prefix is seen by each suffix's workgroup, and there is one launch
 constexpr int64_t kFinishUnits = 256;        // from here on the suffixes alone fill the chip
 constexpr int64_t kJoinRows = 1024;          // from here on a wave joins a row: 4 waves a CU
 
-int32_t splits_of(int64_t keys, int64_t units, int64_t wanted, int32_t* chunk)
+int32_t splits_of(int64_t keys, int64_t units, int64_t wanted, int32_t shortest, int32_t* chunk)
 {
     int64_t n = (wanted + units - 1) / units;
-    if (n > (keys + kMinChunk - 1) / kMinChunk) n = (keys + kMinChunk - 1) / kMinChunk;
+    if (n > (keys + shortest - 1) / shortest) n = (keys + shortest - 1) / shortest;
     if (n > kMaxSplits) n = kMaxSplits;
     if (n < 1) n = 1;
     const int64_t each = ((keys + n - 1) / n + kChunkStep - 1) / kChunkStep * kChunkStep;
@@ -123,7 +126,7 @@ struct Plan {
 };
 
 // Checks a shape and splits its work.  A key range is split until there are two workgroups a CU (three of the form for few rows),
-// in pieces of 256 keys or more; what a suffix may hold at most counts, for its length is known on the device alone.
+// in pieces of kMinChunk keys or more; what a suffix may hold at most counts, for its length is known on the device alone.
 int plan_of(const prefixattn_shape* s, Plan* p)
 {
     if (!s) return fail(ADDRMS_ERR_INVALID_ARG, "shape is NULL");
@@ -183,22 +186,24 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     a.suffix_tiles = static_cast<int32_t>(tiles(own, p->suffix_form));
     const int64_t prefix_units = static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, suffix_units = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads * s->batch;
     const int64_t slots = wanted(p->prefix_form);
-    auto split_prefix = [&](int64_t n) { a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, n, &a.prefix_chunk) : 0; };
+    auto split_prefix = [&](int64_t n) { a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, n, kMinChunk, &a.prefix_chunk) : 0; };
     split_prefix(slots);
     p->finish = suffix && suffix_units >= kFinishUnits && a.prefix_splits <= kFinishSplits;
     if (p->finish && p->suffix_form == FEW) p->suffix_form = few(suffix_units);
     if (suffix) {
-        a.suffix_splits = splits_of(width, suffix_units, p->finish ? 1 : wanted(p->suffix_form), &a.suffix_chunk);
+        a.suffix_splits = splits_of(width, suffix_units, p->finish ? 1 : wanted(p->suffix_form), std::clamp(a.prefix_chunk, kMinChunk, 2 * kMinChunk), &a.suffix_chunk);
         p->suffix_blocks = suffix_units * a.suffix_splits;
         // One launch for both: the prefix leaves the suffixes their places, up to half of all.  Where a workgroup's own pace is the bound
-        // (not with few rows, where memory is), only if its pieces grow by no more keys than a suffix's piece has, which else runs behind
-        // them: 16 x 4 queries over 4001 fp16 keys of 256 and suffixes of 300 take 53.6 us with them behind, 43.4 beside; 8 x 40 heads
-        // over 131072 e4m3 keys and suffixes of 500 75.2 behind, 87.5 beside; with few rows, 4 x 32 heads over 131072 bf16 keys and
-        // suffixes of 2000, 106.0 behind, 103.2 beside.
+        // (not with few rows, where memory is), only if its pieces grow by no more keys than a suffix's piece has, and as many as its
+        // start takes the time of (about kMinChunk), for it else runs behind them: 16 x 4 queries over 4001 fp16 keys of 256 and
+        // suffixes of 300 take 53.6 us with them behind, 42 beside; 8 x 40 heads over 8191 e4m3 keys and one page 19.9 behind, 16.2
+        // beside; over 131072 and suffixes of 500 69 behind, 87 beside; with few rows, 4 x 32 heads over 131072 bf16 keys and
+        // suffixes of 2000, 106 behind, 103 beside.
         if (!p->finish && prefix) {
             const int32_t splits = a.prefix_splits, chunk = a.prefix_chunk;
             split_prefix(std::max(slots / 2, slots - p->suffix_blocks));
-            if (p->prefix_form != FEW && a.prefix_chunk - chunk > std::min<int64_t>(width, a.suffix_chunk)) a.prefix_splits = splits, a.prefix_chunk = chunk;
+            if (p->prefix_form != FEW && a.prefix_chunk - chunk > std::min<int64_t>(width, a.suffix_chunk) + kMinChunk)
+                a.prefix_splits = splits, a.prefix_chunk = chunk;
         }
     }
     p->prefix_blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
