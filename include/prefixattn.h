@@ -45,7 +45,7 @@ typedef struct prefixattn_shape {
 /* Bytes of device memory that a call of this shape keeps partial results in; depends on nothing else. */
 int64_t prefixattn_workspace_bytes(const prefixattn_shape* shape);
 
-/* Asynchronous, two launches.
+/* Asynchronous, one launch or two.
  *   q             device, [batch * q_len, q_heads, d], last axis contiguous, q_strides: host, {token, head}, in elements
  *   k_pages ...   device, as in kvcache.h
  *   prefix_pages  device, int32, at least ceil(prefix_len / page_size); NULL if prefix_len is 0

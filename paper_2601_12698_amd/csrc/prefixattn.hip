@@ -103,9 +103,13 @@ constexpr int64_t kMaxBlocks = 1 << 24;      // of 256 threads: a launch has few
 // 2000 bf16 keys 12.8 and 14.2 us, 2 x 40 over 900 e4m3 10.8 and 11.2, 8 x 40 over 8191 the same; a long prefix with the suffixes in
 // pieces of 128 has too little room left: 4 x 32 heads over 131072 bf16 keys and suffixes of 2000 112 us, with pieces of 256 103.5.
 constexpr int32_t kMinChunk = 128;
-constexpr int64_t kInlineKeys = 512;         // up to here a prefix is seen by each suffix's workgroup, and there is one launch
-constexpr int64_t kFinishUnits = 256;        // from here on the suffixes alone fill the chip
-constexpr int64_t kJoinRows = 1024;          // from here on a wave joins a row: 4 waves a CU
+constexpr int64_t kInlineBytes = 1 << 27, kInlineChain = 3 << 16;      // of keys and values (see plan_of)
+// From here on the suffixes alone fill the chip, and their workgroups join the prefix's parts.  From 64 on instead: 16 x 4 x 32 heads
+// over 4096 fp16 keys and suffixes of 300 32 us a call in place of 25, 8 x 40 heads over 8191 e4m3 keys 28 in place of 16.
+constexpr int64_t kFinishUnits = 256;
+// From here on a wave joins a row, not four: 8192 rows of 128 46.8 us a call in place of 51.5, 2048 26.5 in place of 27.3, 1984 33.0 and
+// 33.7, 1536 30.5 either way; 512 20.8 in place of 19.4.
+constexpr int64_t kJoinRows = 1024;
 
 int32_t splits_of(int64_t keys, int64_t units, int64_t wanted, int32_t shortest, int32_t* chunk)
 {
@@ -125,7 +129,7 @@ struct Plan {
     bool finish;                             // the suffixes' workgroups are a launch of their own that joins the prefix's parts
 };
 
-// Checks a shape and splits its work.  A key range is split until there are two workgroups a CU (three of the form for few rows),
+// Checks a shape and splits its work.  A key range is split until there are as many workgroups as `wanted` says,
 // in pieces of kMinChunk keys or more; what a suffix may hold at most counts, for its length is known on the device alone.
 int plan_of(const prefixattn_shape* s, Plan* p)
 {
@@ -159,25 +163,36 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld queries of %d heads are beyond the limit (2^24 together)", (long long)tokens, s->q_heads);
     p->rows = tokens * s->q_heads;
     const int64_t all = tokens * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
-    auto form_of = [p](int64_t rows) { return rows <= 16 ? FEW : rows <= 64 ? MANY_64 : rows <= 128 || p->dp != 128 ? MANY_128 : MANY_256; };
+    // The least form that has the rows (with 64 rows in 128: 16 x 32 heads over 16384 keys, bf16 25.4 us and 26.0, e4m3 22.2 and 24.0).
+    // Heads over 128 go from 16 to 128: with 16 rows a wave, a form for 64 took 53 us in place of 41 for 20 rows over 16384 bf16 keys
+    // of 256, 54 and 53 for 32, 63 and 59 for 64 (in e4m3 36.5 and 41).
+    auto form_of = [p](int64_t rows) { return rows <= 16 ? FEW : rows <= 64 && p->dp <= 128 ? MANY_64 : rows <= 128 || p->dp != 128 ? MANY_128 : MANY_256; };
     auto tiles = [](int64_t rows, int form) { return (rows + kFormRows[form] - 1) / kFormRows[form]; };
     p->suffix_form = form_of(own);
     p->prefix_form = form_of(all);
     // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
-    // a CU holds one workgroup of eight waves, two of four that share keys, three of those with few rows
-    auto wanted = [p](int form) { return form == FEW ? 768 : form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
+    // A CU holds one workgroup of eight waves and two of four.  (Of few rows three for some types, but 4 x 32 heads over 131072 keys take
+    // 57.4 us with 512, 59.0 with 768, 67.2 with 384 in e4m3, 103.0, 104.0 and 100.5 in bf16, 2 x 32 over 32768 bf16 33.6, 33.9 and 35.6.)
+    auto wanted = [p](int form) { return form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
     // one workgroup a CU, or fewer: eight waves each (32 x 8 heads of e4m3 keys, 16 and then up to 1024: 15.0 us a call with four, 12.5
     // with eight; 64 x 8: 17.6 with four, 21.8 with eight), unless their registers do not suffice (prefixattn_args.h)
     const bool eight = few_8_fits(s->format, p->dp);
     auto few = [eight](int64_t units) { return eight && units <= kFinishUnits ? FEW_8 : FEW; };
-    if (a.pages && a.prefix_len && p->suffix_form == FEW && a.prefix_len <= kInlineKeys &&
-        (static_cast<int64_t>(a.kv_heads) * s->batch >= kFinishUnits || a.prefix_len + width <= 2 * kInlineKeys)) {
-        p->prefix_form = p->suffix_form = few(static_cast<int64_t>(a.kv_heads) * s->batch);
+    // A short prefix is seen by each suffix's workgroup, through the L2s, in one launch: as long as all of them read up to 128 MB of it;
+    // with fewer workgroups than CUs, as long as one reads up to 192 KB with its suffix, or 384 from half the CUs on, for more of them
+    // would then share the work.  32 query and 8 key heads of 128, a prefix and suffixes of 64, one launch and two, us:
+    //   sequences   2 e4m3: 700 keys 9.2, 10.9; 1400 13.0, 10.7   2 bf16: 200 7.5, 9.2; 400 9.3, 9.5; 700 12.1, 9.8
+    //              16 e4m3: 1400 13.6, 13.7                      16 bf16: 400 9.6, 12.6; 700 12.3, 12.5; 1400 19.4, 12.9
+    //              64 e4m3: 700 14.7, 20.5; 1400 22.3, 22.3      64 bf16: 400 14.4, 20.1; 700 19.5, 20.8; 1400 31.7, 23.0
+    const int64_t units = static_cast<int64_t>(a.kv_heads) * s->batch, prefix_bytes = 2 * a.prefix_len * row_bytes, chain = prefix_bytes + 2 * width * row_bytes;
+    if (a.pages && a.prefix_len && p->suffix_form == FEW &&
+        (units >= kFinishUnits ? units * prefix_bytes <= kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain))) {
+        p->prefix_form = p->suffix_form = few(units);
         p->finish = true;
         a.inline_len = a.prefix_len;
         a.suffix_tiles = a.suffix_splits = 1;
         a.suffix_chunk = static_cast<int32_t>(width);
-        p->suffix_blocks = static_cast<int64_t>(a.kv_heads) * s->batch;
+        p->suffix_blocks = units;
         return p->suffix_blocks > kMaxBlocks ? fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)p->suffix_blocks) : ADDRMS_OK;
     }
     const bool prefix = a.prefix_len && a.pages, suffix = width && a.pages;

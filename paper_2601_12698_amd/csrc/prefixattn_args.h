@@ -20,8 +20,8 @@ struct AttnArgs {
     float c;                                          // scale * log2(e): weights are powers of 2
 };
 
-// Forms of a workgroup: 16 rows whose four (FEW_8: eight) waves take keys in turn; 64, 128 or 256 rows that share their keys (256:
-// heads of 65 to 128).
+// Forms of a workgroup: 16 rows whose four (FEW_8: eight) waves take keys in turn; 64, 128 or 256 rows that share their keys (64:
+// heads up to 128; 256: heads of 65 to 128).
 enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2, MANY_256 = 3, FEW_8 = 4 };
 // Eight waves have 256 registers each.  Heads over 128 in 16 bits would spill 62 of them (32 x 8 heads of 256 over 500 fp16 keys at
 // most: 23.1 us with four waves, 32.4 with eight).

@@ -12,9 +12,26 @@
 // O is scaled down only when a maximum grows by more than 2^8 (weights stay below that, and l and O are relative to the same
 // number): most tiles leave 16 to 128 multiplications a lane out.
 //
-// Two forms.  FEW (up to 16 rows): every wave has all rows and takes every fourth tile of 32 keys by itself, keys straight from
-// memory into registers, values through LDS of its own, no barrier until the waves' results are joined.  MANY: each of four waves
-// has 32 rows, the tile of 64 keys and values is staged in LDS for all of them, two tiles deep.
+// FEW (up to 16 rows; four or eight waves): every wave has all rows and takes every fourth (eighth) tile of 32 keys by itself, keys straight
+// from memory into registers, values through LDS of its own, no barrier until the waves' results are joined.  Bound by memory:
+// 4 x 32 heads over 131072 bf16 keys of 128, 537 MB in 95 us, 5.6 TB/s (e4m3 270 MB in 54 us).
+//
+// MANY (64, 128 or 256 rows): the tile of keys and values is staged in LDS for all waves, as elements, two tiles deep, and asked for
+// two turns before that.  A wave has 32 rows and all keys of the tile; where there are 64 rows, two waves share rows and halve the
+// keys, and are joined at the end (16 rows a wave and all keys: each wave reads all of the tile from LDS, 8 x 40 heads over 131072
+// e4m3 keys 87 us a call, so 70).  More rows a workgroup mean fewer reads of a head's keys: 256 rows read a tile from LDS once for
+// 128 operations a byte, one workgroup a CU.  Heads over 128 leave no registers for 32 rows a wave (32 x 256 sums are half of them):
+// 16 rows, eight waves.
+//   64 x 64 heads over 32768 e4m3 keys, 69 GFLOP: 85 to 93 us, 740 to 810 TFLOP/s, of 1211 that a large matrix product reaches here
+//   (and 1340 of matrix instructions alone: power is the limit).  What is between is the softmax: exponentials, conversions and maxima
+//   are as many cycles as the products, and waves that share a SIMD overlap them in part.  16 x 4 x 32 heads of 256 over 65536
+//   fp16 keys: 575 TFLOP/s.
+// Tried at the 256-row form and not faster: the next tile's scores before this one's sums, 64 rows a wave, half the waves a phase
+// behind, wave priorities, fixed instruction orders.  At heads of 256, two waves that share weights through LDS and halve the elements
+// of O: half the LDS reads, two barriers a tile, 3 to 7 % faster over 65536 keys and up to 6 % slower over 4001.
+//
+// A short prefix is seen by each suffix's workgroup before its own keys (`turn`): one launch.  Where the suffixes'
+// workgroups fill the chip, they join the prefix's parts themselves (`finish`): two launches.  Else the joining kernel does.
 #pragma once
 #include "kvcache.h"
 #include "prefixattn_args.h"
@@ -414,7 +431,7 @@ struct Many {
     typedef typename M::T8 T8;
     static constexpr bool CODES = FORMAT == KVCACHE_E4M3, WIDE = RW == 32;
     static constexpr int ES = CODES ? 1 : 2, THREADS = 64 * WAVES, GROUPS = WAVES / KS, ROWS = RW * GROUPS;
-    static constexpr int TILE = DP > 128 && WAVES == 4 ? 32 : 64;   // keys at a time: two workgroups' tiles, or one of eight waves, fit a CU
+    static constexpr int TILE = 64;                             // keys at a time: two workgroups' tiles, or one of eight waves, fit a CU
     static constexpr int KEYS = TILE / KS;                      // of a wave
     typedef typename acc<RW>::type A;                           // of a lane: WIDE 16 of 32 keys (or elements) by rows, else 4 of 16
     static constexpr int AN = WIDE ? 16 : 4;
@@ -698,7 +715,7 @@ template <int DP> constexpr int threads_of(int form) { return form == FEW_8 || f
 template <int DT, int FORMAT, int DP, int FORM, int WAVES> struct form;
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW, WAVES> { typedef Few<DT, FORMAT, DP, WAVES> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW_8, WAVES> { typedef Few<DT, FORMAT, DP, 8> type; };
-template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_64, WAVES> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), 4, (DP > 128 ? 1 : 2)> type; };
+template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_64, WAVES> { typedef Many<DT, FORMAT, DP, 32, 4, 2> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_128, WAVES> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4)> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8> type; };
 

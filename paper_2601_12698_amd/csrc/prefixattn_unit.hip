@@ -18,7 +18,10 @@ hipError_t ATTN_UNIT(UNIT_DT, UNIT_FORMAT, UNIT_DP)(const AttnArgs& a, int prefi
     if constexpr (few_8_fits(UNIT_FORMAT, UNIT_DP))
         if (prefix_form == FEW_8) return launch<FEW_8, FEW_8>(a, blocks, s);
     if (prefix_form == FEW) return launch<FEW, FEW>(a, blocks, s);
-    if (prefix_form == MANY_64) return suffix_form == FEW ? launch<MANY_64, FEW>(a, blocks, s) : launch<MANY_64, MANY_64>(a, blocks, s);
+    if constexpr (UNIT_DP <= 128) {
+        if (prefix_form == MANY_64) return suffix_form == FEW ? launch<MANY_64, FEW>(a, blocks, s) : launch<MANY_64, MANY_64>(a, blocks, s);
+        if (prefix_form == MANY_128 && suffix_form == MANY_64) return launch<MANY_128, MANY_64>(a, blocks, s);
+    }
 #if UNIT_DP == 128
     if (prefix_form == MANY_256) {
         if (suffix_form == FEW) return launch<MANY_256, FEW>(a, blocks, s);
@@ -26,8 +29,7 @@ hipError_t ATTN_UNIT(UNIT_DT, UNIT_FORMAT, UNIT_DP)(const AttnArgs& a, int prefi
         return suffix_form == MANY_128 ? launch<MANY_256, MANY_128>(a, blocks, s) : launch<MANY_256, MANY_256>(a, blocks, s);
     }
 #endif
-    if (suffix_form == FEW) return launch<MANY_128, FEW>(a, blocks, s);
-    return suffix_form == MANY_64 ? launch<MANY_128, MANY_64>(a, blocks, s) : launch<MANY_128, MANY_128>(a, blocks, s);
+    return suffix_form == FEW ? launch<MANY_128, FEW>(a, blocks, s) : launch<MANY_128, MANY_128>(a, blocks, s);
 }
 
 }  // namespace serving

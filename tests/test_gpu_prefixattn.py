@@ -263,8 +263,8 @@ def test_on_another_stream_and_in_a_graph_with_growing_suffixes(short):
 
 
 def test_one_workspace_after_the_other_and_refused_where_small():
-    c, dtype = build((2, 1, 8, 2, 128, 600, [5, 16], 1, 16, "bf16", True), seed=1)
-    shape = S.prefixattn_shape(2, 1, 8, 2, 128, 16, c["k_pages"].shape[0], 600, 1, dtype, True)
+    c, dtype = build((2, 1, 8, 2, 128, 1600, [5, 16], 1, 16, "bf16", True), seed=1)
+    shape = S.prefixattn_shape(2, 1, 8, 2, 128, 16, c["k_pages"].shape[0], 1600, 1, dtype, True)
     n = S.prefixattn_workspace_bytes(shape)
     with pytest.raises(S.AddrmsError, match="workspace has"):
         call(c, dtype, workspace=torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
