@@ -184,7 +184,9 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     //   sequences   2 e4m3: 700 keys 9.2, 10.9; 1400 13.0, 10.7   2 bf16: 200 7.5, 9.2; 400 9.3, 9.5; 700 12.1, 9.8
     //              16 e4m3: 1400 13.6, 13.7                      16 bf16: 400 9.6, 12.6; 700 12.3, 12.5; 1400 19.4, 12.9
     //              64 e4m3: 700 14.7, 20.5; 1400 22.3, 22.3      64 bf16: 400 14.4, 20.1; 700 19.5, 20.8; 1400 31.7, 23.0
-    const int64_t units = static_cast<int64_t>(a.kv_heads) * s->batch, prefix_bytes = 2 * a.prefix_len * row_bytes, chain = prefix_bytes + 2 * width * row_bytes;
+    // (a key counts for 256 bytes at least: less is not faster)
+    const int64_t units = static_cast<int64_t>(a.kv_heads) * s->batch, key_bytes = std::max(256, 2 * p->dp * (s->format == KVCACHE_E4M3 ? 1 : 2));
+    const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
     if (a.pages && a.prefix_len && p->suffix_form == FEW &&
         (units >= kFinishUnits ? units * prefix_bytes <= kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain))) {
         p->prefix_form = p->suffix_form = few(units);
