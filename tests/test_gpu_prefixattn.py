@@ -119,6 +119,15 @@ CASES = [
     (65, 18, 16, 4, 96, 257, [(9 * i) % 40 for i in range(65)], 3, 16, "bf16", False),
     (64, 25, 24, 4, 128, 65, [(13 * i) % 90 for i in range(64)], 6, 16, "bf16", True),
     (86, 20, 21, 3, 64, 200, [(7 * i) % 60 for i in range(86)], 4, 16, "fp16", True),
+    # the same with few rows, with four waves and with eight
+    (130, 1, 8, 2, 128, 2100, [(7 * i) % 41 - 1 for i in range(130)], 3, 16, "bf16", True),
+    (64, 1, 16, 4, 64, 2150, [(7 * i) % 41 - 1 for i in range(64)], 3, 16, "bf16", True),
+    (64, 2, 12, 4, 112, 1100, [(5 * i) % 35 for i in range(64)], 2, 16, "fp16", False),
+    (129, 1, 6, 2, 256, 600, [(3 * i) % 17 for i in range(129)], 1, 16, "fp16", False),
+    # longer prefixes that the suffixes' workgroups see: by four waves and by eight
+    (130, 1, 8, 2, 64, 1999, [(7 * i) % 41 - 1 for i in range(130)], 3, 16, "bf16", True),
+    (64, 1, 16, 4, 64, 2047, [(7 * i) % 41 - 1 for i in range(64)], 3, 16, "fp16", False),
+    (36, 3, 8, 4, 128, 701, [(7 * i) % 33 - 1 for i in range(36)], 2, 16, "bf16", False),
 ]
 
 

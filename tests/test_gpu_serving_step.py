@@ -91,9 +91,9 @@ def test_native_and_general_calls_agree(monkeypatch):
         assert torch.equal(got, ref)
     monkeypatch.undo()
     cache = [torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16, device=dev) for _ in range(2)] + [None, None]
-    long = [torch.zeros(40, 2, 16, 64, dtype=torch.bfloat16, device=dev) for _ in range(2)] + [None, None]
+    long = [torch.zeros(90, 2, 16, 64, dtype=torch.bfloat16, device=dev) for _ in range(2)] + [None, None]
     with pytest.raises(S.AddrmsError, match="workspace has"):
-        S.prefixattn_run(q, *long, torch.zeros(40, dtype=torch.int32, device=dev), 640, None, None, torch.empty(6, 8, 64, dtype=torch.bfloat16, device=dev),
+        S.prefixattn_run(q, *long, torch.zeros(90, dtype=torch.int32, device=dev), 1440, None, None, torch.empty(6, 8, 64, dtype=torch.bfloat16, device=dev),
                          None, 0.125, "bf16", workspace=torch.empty(4, dtype=torch.uint8, device=dev))
     with pytest.raises(ValueError, match="has shape"):
         S.rotary_run(q, k, torch.empty_like(k), torch.empty_like(k), pos, freq, axis, "bf16")

@@ -120,18 +120,18 @@ def test_attention_without_work_and_unknown_shapes():
 
 
 def test_workspace_holds_a_part_for_each_split():
-    """4 d + 8 bytes for each row and part; the parts of a range never hold less than 256 keys but for the last.  Suffixes that fill
+    """4 d + 8 bytes for each row and part; the parts of a range never hold less than 128 keys but for the last.  Suffixes that fill
     the chip by themselves join the prefix's parts to their own and have none, and where they also see a short prefix there is no part."""
     for prefix, width in ((0, 4), (1, 0), (256, 0), (257, 4), (100000, 100), (1 << 20, 1 << 10)):
         for batch, q_len, heads in ((1, 1, (1, 1)), (64, 1, (64, 8)), (3, 40, (8, 2))):
             s = shape(batch=batch, q_len=q_len, q_heads=heads[0], kv_heads=heads[1], prefix_len=prefix, suffix_width=width, pages=1 << 20)
             rows, n = batch * q_len * heads[0], S.prefixattn_workspace_bytes(s)
             if n == 0:
-                assert prefix <= 512 and q_len * heads[0] // heads[1] <= 16
+                assert prefix <= 1024 and q_len * heads[0] // heads[1] <= 16
                 continue
             assert n % (rows * (4 * 128 + 8)) == 0
             parts = n // (rows * (4 * 128 + 8))
-            assert (prefix > 0) + (width > 0 and batch * heads[1] < 256) <= parts <= -(-prefix // 256) + -(-width * 16 // 256)
+            assert (prefix > 0) + (width > 0 and batch * heads[1] < 256) <= parts <= -(-prefix // 128) + -(-width * 16 // 128)
 
 
 def test_bytes_formulas():
