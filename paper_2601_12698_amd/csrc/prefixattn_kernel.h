@@ -442,11 +442,13 @@ struct Many {
     static constexpr int PIECES = DP * ES / 16;
     static constexpr int NP = TILE * PIECES / THREADS;          // 16-byte pieces of keys, and of values, that a thread stages
     static_assert(NP >= 1, "fewer pieces than threads");
-    // Bytes from key to key in LDS: lanes that are served together fall on different banks, 8 or 16 keys' 16 bytes for the keys,
-    // and for a transposing read of the values 4 keys' 64 bytes (WIDE) or 8 keys' 32.
-    static constexpr int KROW = DP * 2 + 16, VROW = DP * 2 + (WIDE ? 64 : 32);
+    // Bytes from key to key in LDS: lanes that are served together fall on different banks, for the keys 16 bytes of 16 keys (WIDE) or
+    // 32 of 8, and for a transposing read of the values 4 keys' 64 bytes (WIDE) or 8 keys' 32.  (16 rows a wave with 16 bytes between
+    // the keys: a quarter of the LDS's time goes to conflicts, and 16 x 4 x 32 heads of 256 over 65536 fp16 keys take 260 us, not 249.)
+    static constexpr int KROW = DP * 2 + (WIDE ? 16 : 32), VROW = DP * 2 + (WIDE ? 64 : 32);
     static constexpr int BUF = TILE * (KROW + VROW) + TILE;     // keys, values, a byte for each key that is there
     static constexpr int LDS = 2 * BUF;
+    static constexpr bool ONE = DP > 128;                       // one set of pieces on their way
 
     static __device__ __forceinline__ int key_of(int i) { return (THREADS / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
     static __device__ __forceinline__ int piece() { return static_cast<int>(threadIdx.x) % PIECES; }
@@ -591,47 +593,47 @@ struct Many {
         };
 
         if (s.first < s.end) {
-            // Tiles are asked for two turns before they are staged (a turn is shorter than memory takes), in two sets of registers.
+            // Tiles are asked for two turns before they are staged (a turn is shorter than memory takes), in two sets of registers.  Heads
+            // over 128 have longer turns and no registers for that: one set, asked for again as soon as it is staged.
+            // Page numbers are asked for before the pieces, and both in every turn, also for tiles that are beyond the end (whose keys
+            // then are not there): loads come back in their order and are waited for by their number, so that a page number behind its
+            // turn's pieces, or loads in a branch, would make every wait one for the newest.
             Staged even, odd;
             int32_t page[NP];
-            pages_of(a, s, s.first, page);
-            even.load(a, s, s.first, page);
-            pages_of(a, s, s.first + TILE, page);
-#pragma unroll
-            for (int c = 0; c < NC; ++c) q[c] = query_piece<DT>(a, row, KC * c + 8 * g);
-            {
+            const auto ask = [&](Staged& to, int32_t key0) {
                 int32_t now[NP];
 #pragma unroll
                 for (int i = 0; i < NP; ++i) now[i] = page[i];
-                pages_of(a, s, s.first + 2 * TILE, page);
-                odd.load(a, s, s.first + TILE, now);
-            }
+                pages_of(a, s, key0 + TILE, page);
+                to.load(a, s, key0, now);
+            };
+            pages_of(a, s, s.first, page);
+            ask(even, s.first);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) q[c] = query_piece<DT>(a, row, KC * c + 8 * g);
+            if constexpr (!ONE) ask(odd, s.first + TILE);
             even.clear(a);
             even.stage(lds);
+            if constexpr (ONE) ask(even, s.first + TILE);
             __syncthreads();
             // one turn: `key0`'s tile is in `buf`, the next one arrives in `next`, the one after is asked for into `after`
             const auto turn = [&](int32_t key0, char* buf, char* other, Staged& next, Staged& after) {
-                // Page numbers are asked for before the pieces, and both in every turn, also for tiles that are beyond the end (whose keys
-                // then are not there): loads come back in their order and are waited for by their number, so that a page number behind
-                // its turn's pieces, or loads in a branch, would make every wait one for the newest.
-                int32_t now[NP];
-#pragma unroll
-                for (int i = 0; i < NP; ++i) now[i] = page[i];
-                pages_of(a, s, key0 + 3 * TILE, page);
-                after.load(a, s, key0 + 2 * TILE, now);
+                if constexpr (!ONE) ask(after, key0 + 2 * TILE);
                 if (busy) attend(buf, key0);
                 if (key0 + TILE < s.end) {
                     next.clear(a);
                     next.stage(other);
                 }
+                if constexpr (ONE) ask(after, key0 + 2 * TILE);
                 __syncthreads();
             };
+            Staged& second = ONE ? even : odd;
             int32_t key0 = s.first;
             for (; key0 + TILE < s.end; key0 += 2 * TILE) {
-                turn(key0, lds, lds + BUF, odd, even);
-                turn(key0 + TILE, lds + BUF, lds, even, odd);
+                turn(key0, lds, lds + BUF, second, even);
+                turn(key0 + TILE, lds + BUF, lds, even, second);
             }
-            if (key0 < s.end) turn(key0, lds, lds + BUF, odd, even);
+            if (key0 < s.end) turn(key0, lds, lds + BUF, second, even);
         }
         if constexpr (KS == 2) {
             // what the waves of a tile's other half found, register by register
