@@ -25,7 +25,7 @@
 //   64 x 64 heads over 32768 e4m3 keys, 69 GFLOP: 85 to 93 us, 740 to 810 TFLOP/s, of 1211 that a large matrix product reaches here
 //   (and 1340 of matrix instructions alone: power is the limit).  What is between is the softmax: exponentials, conversions and maxima
 //   are as many cycles as the products, and waves that share a SIMD overlap them in part.  16 x 4 x 32 heads of 256 over 65536
-//   fp16 keys: 575 TFLOP/s.
+//   fp16 keys: 600 TFLOP/s.
 // Tried at the 256-row form and not faster: the next tile's scores before this one's sums, 64 rows a wave, half the waves a phase
 // behind, wave priorities, fixed instruction orders.  At heads of 256, two waves that share weights through LDS and halve the elements
 // of O: half the LDS reads, two barriers a tile, 3 to 7 % faster over 65536 keys and up to 6 % slower over 4001.
@@ -542,6 +542,18 @@ struct Many {
                 z[t] = A{};
 #pragma unroll
                 for (int c = 0; c < NC; ++c) z[t] = mul(*reinterpret_cast<const T8*>(kt + RW * t * KROW + 2 * KC * c), q[c], z[t]);
+            }
+            // Four of LDS's answers under way, then one asked for with each matrix instruction (left to the compiler, two at a time and
+            // both waited for: 16 x 4 x 32 heads of 256 over 65536 fp16 keys 245 us, so 238; 64 x 64 of 128 over 32768 e4m3 91.9 and 90.8;
+            // heads of 64, with four instructions a piece, are 1 % slower so).
+            if constexpr (DP > 64) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                for (int i = 4; i < NS * NC; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
             }
             const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane % TILE] != 0) & full_of(TILE);
             if (there != full_of(TILE) || key0 + TILE - 1 > s.last0) {
