@@ -175,9 +175,8 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // 57.4 us with 512, 59.0 with 768, 67.2 with 384 in e4m3, 103.0, 104.0 and 100.5 in bf16, 2 x 32 over 32768 bf16 33.6, 33.9 and 35.6.)
     auto wanted = [p](int form) { return form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
     // one workgroup a CU, or fewer: eight waves each (32 x 8 heads of e4m3 keys, 16 and then up to 1024: 15.0 us a call with four, 12.5
-    // with eight; 64 x 8: 17.6 with four, 21.8 with eight), unless their registers do not suffice (prefixattn_args.h)
-    const bool eight = few_8_fits(s->format, p->dp);
-    auto few = [eight](int64_t units) { return eight && units <= kFinishUnits ? FEW_8 : FEW; };
+    // with eight; 64 x 8: 17.6 with four, 21.8 with eight)
+    auto few = [](int64_t units) { return units <= kFinishUnits ? FEW_8 : FEW; };
     // A short prefix is seen by each suffix's workgroup, through the L2s, in one launch: as long as all of them read up to 128 MB of it;
     // with fewer workgroups than CUs, as long as one reads up to 192 KB with its suffix, or 384 from half the CUs on, for more of them
     // would then share the work.  32 query and 8 key heads of 128, a prefix and suffixes of 64, one launch and two, us:

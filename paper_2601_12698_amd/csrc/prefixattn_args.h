@@ -23,9 +23,6 @@ struct AttnArgs {
 // Forms of a workgroup: 16 rows whose four (FEW_8: eight) waves take keys in turn; 64, 128 or 256 rows that share their keys (64:
 // heads up to 128; 256: heads of 65 to 128).
 enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2, MANY_256 = 3, FEW_8 = 4 };
-// Eight waves have 256 registers each.  Heads over 128 in 16 bits would spill 62 of them (32 x 8 heads of 256 over 500 fp16 keys at
-// most: 23.1 us with four waves, 32.4 with eight).
-constexpr bool few_8_fits(int format, int dp) { return format != 0 || dp <= 128; }
 constexpr int kJoinThreads = 256;
 constexpr int kFormRows[] = {16, 64, 128, 256, 16};
 constexpr int kChunkStep = 128;                       // splits begin at multiples of this many keys: every tile is aligned

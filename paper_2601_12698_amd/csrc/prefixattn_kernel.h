@@ -178,7 +178,13 @@ struct Few {
     static constexpr int VROW = DP * 2 + 32;                    // bytes from key to key in LDS: 4 keys' 32 bytes fall on 4 groups of banks
     static constexpr int WAVE_LDS = TILE * VROW;
     static constexpr int OROW = DP + 4;                         // floats from row to row where waves are joined
-    static constexpr int LDS = WAVES * (WAVE_LDS > ROWS * OROW * 4 ? WAVE_LDS : ROWS * OROW * 4);
+    static constexpr int JOIN_LDS = WAVES * (WAVE_LDS > ROWS * OROW * 4 ? WAVE_LDS : ROWS * OROW * 4);
+    // Eight waves' 256 registers do not hold keys and values of 32 x 256 elements in 16 bits, sums and queries: the queries stay in LDS,
+    // and what follows from the lane is made anew in every turn (32 x 8 heads over 500 fp16 keys at most 20.5 us, with queries and
+    // all of that in registers and scratch memory 32.4; beside a prefix's workgroups, 16 x 4 queries over 4001 39.0 in place of 41.1).
+    static constexpr bool Q_LDS = !CODES && DP > 128 && WAVES == 8;
+    static constexpr int QROW = DP * 2 + 32;
+    static constexpr int LDS = JOIN_LDS + (Q_LDS ? ROWS * QROW : 0);
 
     u32x4 k[2][NK], v[NV];
     uint32_t k_scale, v_scale;                                  // of key lane % 32
@@ -245,6 +251,12 @@ struct Few {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
         const Row row = row_of(a, s, lane & 15);
         T8 q[NC];
+        const char* const at_q = lds + JOIN_LDS + (lane & 15) * QROW + 16 * g;
+        if constexpr (Q_LDS) {
+            static_assert(NC == WAVES, "a wave brings one piece of the queries");
+            *reinterpret_cast<T8*>(lds + JOIN_LDS + (lane & 15) * QROW + 64 * wave + 16 * g) = query_piece<DT>(a, row, 32 * wave + 8 * g);
+            __syncthreads();
+        } else
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int32_t e = CODES ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
@@ -265,11 +277,15 @@ struct Few {
             page = page_of(a, s, key0 + WAVES * TILE, lane);
         }
         while (key0 < s.end) {
-            clear(a, lane);
+            // made anew in every turn, so that what follows from it is not held in registers (from where it would go to scratch memory,
+            // whose loads wait for those of keys and values)
+            int here = lane;
+            if constexpr (Q_LDS) asm volatile("" : "+v"(here));
+            clear(a, here);
             // values to LDS, as elements
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int at = (64 / PIECES) * i + lane / PIECES, b = lane % PIECES;
+                const int at = (64 / PIECES) * i + here / PIECES, b = here % PIECES;
                 if constexpr (CODES) {
                     const float sc = scale_of(__shfl(v_scale, at));
                     T8* to = reinterpret_cast<T8*>(mine + at * VROW + 32 * b);
@@ -293,15 +309,15 @@ struct Few {
                     }
                 } else {
 #pragma unroll
-                    for (int c = 0; c < NK; ++c) z[t] = M::mul16(__builtin_bit_cast(T8, k[t][c]), q[c], z[t]);
+                    for (int c = 0; c < NK; ++c) z[t] = M::mul16(__builtin_bit_cast(T8, k[t][c]), Q_LDS ? *reinterpret_cast<const T8*>(at_q + 64 * c) : q[c], z[t]);
                 }
             }
             const uint32_t there = valid;
             const int32_t now = key0;
             key0 += WAVES * TILE;
             if (key0 < s.end) {
-                load(a, s, key0, page, lane);
-                page = page_of(a, s, key0 + WAVES * TILE, lane);
+                load(a, s, key0, page, here);
+                page = page_of(a, s, key0 + WAVES * TILE, here);
             }
             if (there != 0xffffffffu || now + TILE - 1 > s.last0) {
                 const uint32_t mine_there = there >> (4 * g);   // this lane's keys, shifted so that each is a fixed bit

@@ -15,8 +15,7 @@ hipError_t launch(const AttnArgs& a, unsigned blocks, hipStream_t s)
 // A sequence's rows are some of the prefix's rows, so that its form is never the larger one.
 hipError_t ATTN_UNIT(UNIT_DT, UNIT_FORMAT, UNIT_DP)(const AttnArgs& a, int prefix_form, int suffix_form, unsigned blocks, hipStream_t s)
 {
-    if constexpr (few_8_fits(UNIT_FORMAT, UNIT_DP))
-        if (prefix_form == FEW_8) return launch<FEW_8, FEW_8>(a, blocks, s);
+    if (prefix_form == FEW_8) return launch<FEW_8, FEW_8>(a, blocks, s);
     if (prefix_form == FEW) return launch<FEW, FEW>(a, blocks, s);
     if constexpr (UNIT_DP <= 128) {
         if (prefix_form == MANY_64) return suffix_form == FEW ? launch<MANY_64, FEW>(a, blocks, s) : launch<MANY_64, MANY_64>(a, blocks, s);
