@@ -101,6 +101,15 @@ __device__ __forceinline__ float other_half_sum(float x) { const pair p = with_h
 __device__ __forceinline__ float other_row_max(float x) { const pair p = with_row(x); return larger(p.a, p.b); }
 __device__ __forceinline__ float other_row_sum(float x) { const pair p = with_row(x); return p.a + p.b; }
 
+// The thread's number; ANEW: as if it had not been known, so that what follows from it is not held in registers meanwhile.
+template <bool ANEW>
+__device__ __forceinline__ int thread()
+{
+    int t = threadIdx.x;
+    if constexpr (ANEW) asm volatile("" : "+v"(t));
+    return t;
+}
+
 // A workgroup's share: rows [row0, row0 + rows) of a key head, rows counted token by token from token `token0`, keys
 // [first, end) of a table of pages.  Query i of its sequence sees keys up to last0 + i.
 // Keys from `turn` on are those of a second table, counted from 0 there (a short prefix, then a suffix; kAll: none).
@@ -180,8 +189,9 @@ struct Few {
     static constexpr int OROW = DP + 4;                         // floats from row to row where waves are joined
     static constexpr int JOIN_LDS = WAVES * (WAVE_LDS > ROWS * OROW * 4 ? WAVE_LDS : ROWS * OROW * 4);
     // Eight waves' 256 registers do not hold keys and values of 32 x 256 elements in 16 bits, sums and queries: the queries stay in LDS,
-    // and what follows from the lane is made anew in every turn (32 x 8 heads over 500 fp16 keys at most 20.5 us, with queries and
-    // all of that in registers and scratch memory 32.4; beside a prefix's workgroups, 16 x 4 queries over 4001 39.0 in place of 41.1).
+    // what follows from the lane is made anew in every turn and after the last, and the places of values are scalars until they are
+    // loaded from (32 x 8 heads over a page and 500 fp16 keys at most 19.1 us; with a place for each lane, and so scratch memory between
+    // the loads, 22.4; with the queries in registers, too, 32.4).
     static constexpr bool Q_LDS = !CODES && DP > 128 && WAVES == 8;
     static constexpr int QROW = DP * 2 + 32;
     static constexpr int LDS = JOIN_LDS + (Q_LDS ? ROWS * QROW : 0);
@@ -220,8 +230,17 @@ struct Few {
         const int32_t b = 16 * (lane % PIECES);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = (64 / PIECES) * i + lane / PIECES;
-            v[i] = *reinterpret_cast<const u32x4*>(vp + place_of(a, s.head, __shfl(page, at), local(s, key0 + at), row_bytes).bytes + (b < row_bytes ? b : 0));
+            uint64_t from;
+            if constexpr (PIECES == 32) {                       // two keys a load, one for each half of the lanes: their places are scalars
+                const int32_t first = __builtin_amdgcn_readfirstlane(key0) + 2 * i;
+                const uint64_t lo = place_of(a, s.head, __builtin_amdgcn_readlane(page, 2 * i), local(s, first), row_bytes).bytes;
+                const uint64_t hi = place_of(a, s.head, __builtin_amdgcn_readlane(page, 2 * i + 1), local(s, first + 1), row_bytes).bytes;
+                from = lane < 32 ? lo : hi;
+            } else {
+                const int at = (64 / PIECES) * i + lane / PIECES;
+                from = place_of(a, s.head, __shfl(page, at), local(s, key0 + at), row_bytes).bytes;
+            }
+            v[i] = *reinterpret_cast<const u32x4*>(vp + from + (b < row_bytes ? b : 0));
         }
     }
     // Zeros in the place of keys that are not there and of elements beyond the head.
@@ -245,8 +264,8 @@ struct Few {
         return page_at(a, s, min(key0 + (lane & 31), s.end - 1));
     }
 
-    // `page0`: that of key lane % 32 of this wave's first tile.
-    __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, int32_t page0, char* lds)
+    // Over the share's keys: sums O, maximum and sum of weights of this wave's tiles.  `page0`: that of key lane % 32 of the first.
+    __device__ __forceinline__ void pass(const AttnArgs& a, const Share& s, int32_t page0, char* lds, f32x4 (&o)[DP / 16], float& m, float& l)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
         const Row row = row_of(a, s, lane & 15);
@@ -262,10 +281,9 @@ struct Few {
             const int32_t e = CODES ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
             q[c] = query_piece<DT>(a, row, e);
         }
-        f32x4 o[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = f32x4{0, 0, 0, 0};
-        float m = kNone, l = 0.0f;
+        m = kNone, l = 0.0f;
         const float lag = fminf(kLazy / a.c, kMost);
         char* mine = lds + wave * WAVE_LDS;
         // where this lane's 8 bytes of a transposing read begin: key 4 g + (lane % 16) / 4 of 16, elements 4 (lane % 4) of 16
@@ -279,8 +297,7 @@ struct Few {
         while (key0 < s.end) {
             // made anew in every turn, so that what follows from it is not held in registers (from where it would go to scratch memory,
             // whose loads wait for those of keys and values)
-            int here = lane;
-            if constexpr (Q_LDS) asm volatile("" : "+v"(here));
+            const int here = thread<Q_LDS>() & 63;
             clear(a, here);
             // values to LDS, as elements
 #pragma unroll
@@ -358,8 +375,17 @@ struct Few {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
+    }
+
+    __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, int32_t page0, char* lds)
+    {
+        f32x4 o[NT];
+        float m, l;
+        pass(a, s, page0, lds, o, m, l);
 
         // the waves' results, joined
+        const int tid = thread<true>(), lane = tid & 63, wave = tid >> 6, g = lane >> 4;
+        const Row row = row_of(a, s, lane & 15);
         l = other_half_sum(other_row_sum(l));
         __shared__ float2 ml[WAVES][ROWS];
         if (lane < 16) ml[wave][lane] = make_float2(m, l);
