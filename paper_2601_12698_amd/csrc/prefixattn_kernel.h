@@ -101,6 +101,62 @@ __device__ __forceinline__ float other_half_sum(float x) { const pair p = with_h
 __device__ __forceinline__ float other_row_max(float x) { const pair p = with_row(x); return larger(p.a, p.b); }
 __device__ __forceinline__ float other_row_sum(float x) { const pair p = with_row(x); return p.a + p.b; }
 
+// Values that are no finite numbers, of keys that some rows of a tile see and others do not.  A weight of zero does not take such a
+// value out of a product.  A share that holds such keys looks at its sums when it is done, and if one is not finite goes over its keys
+// again with SAFE: the value becomes a zero in LDS, and `first` keeps, for each element, the first key at which it was NaN, +inf or
+// -inf.  Rows see the keys up to a last one: those from that first key on get the value added to their sum.  Looking at the sums costs
+// a meeting of the waves, where there are several queries a sequence: 2 x 64 queries of 32 heads over 1000 and 1000 keys 0.4 us of 17
+// (e4m3, heads of 64), 1 of 39 (bf16, 256).  Looking through every such tile as it is staged takes 2 of 17 and 3 of 39.
+template <int DT, int DP>
+struct Strays {
+    static constexpr uint32_t EXPONENT = DT == DT_BF16 ? 0x7f80u : 0x7c00u;
+    int32_t first[3][DP];
+    int32_t odd[16];                                            // of each wave: a sum was not finite
+
+    // Whether the workgroup has to go over its keys again; if so, ready for that.
+    template <int WAVES, int N, typename V>
+    __device__ __forceinline__ bool found(const V (&o)[N], int wave, bool mine)
+    {
+        constexpr int EACH = sizeof(V) / 4;
+        float none[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) none[i % 4] = __builtin_fmaf(o[t][i], 0.0f, none[i % 4]);
+        const float all = (none[0] + none[1]) + (none[2] + none[3]);
+        const bool some = __any(mine && all != all);
+        if (threadIdx.x % 64 == 0) odd[wave] = some;
+        __syncthreads();
+        int32_t any = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) any |= odd[w];
+        if (__builtin_expect(any == 0, 1)) return false;
+        for (int i = threadIdx.x; i < 3 * DP; i += 64 * WAVES) first[0][i] = 0x7fffffff;
+        __syncthreads();
+        return true;
+    }
+    // Eight elements in LDS, those of `key` from e on.
+    __device__ __forceinline__ void take_out(char* at, int32_t key, int32_t e)
+    {
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+            uint16_t* p = reinterpret_cast<uint16_t*>(at) + i;
+            const uint32_t w = *p;
+            if ((w & EXPONENT) != EXPONENT) continue;
+            const int kind = (w & (EXPONENT ^ 0x7fffu)) ? 0 : w >> 15 ? 2 : 1;
+            atomicMin(&first[kind][e + i], key);
+            *p = 0;
+        }
+    }
+    // What element e of a row's sum gets.
+    __device__ __forceinline__ float of(int32_t e, int32_t last) const
+    {
+        float x = first[1][e] <= last ? __builtin_huge_valf() : 0.0f;
+        x = first[2][e] <= last ? x - __builtin_huge_valf() : x;
+        return first[0][e] <= last ? __builtin_nanf("") : x;
+    }
+};
+
 // The thread's number; ANEW: as if it had not been known, so that what follows from it is not held in registers meanwhile.
 template <bool ANEW>
 __device__ __forceinline__ int thread()
@@ -116,8 +172,15 @@ __device__ __forceinline__ int thread()
 struct Share {
     addr_t table, table2;
     int32_t turn, head, token0, row0, rows, first, end, part, last0;
+    int32_t sure;                                               // all rows see the keys up to this one; kAll if those are all
 };
 constexpr int32_t kAll = 0x7fffffff;
+// A suffix's `sure`, once its other members are set: the last key of the tile's first row.
+__device__ __forceinline__ int32_t sure_of(const AttnArgs& a, const Share& s)
+{
+    const int32_t last = max(s.last0 + s.row0 / a.group, s.turn < kAll ? s.turn - 1 : -1);
+    return last >= s.end - 1 ? kAll : last;
+}
 __device__ __forceinline__ int32_t page_at(const AttnArgs& a, const Share& s, int32_t key)
 {
     const bool second = key >= s.turn;
@@ -195,6 +258,18 @@ struct Few {
     static constexpr bool Q_LDS = !CODES && DP > 128 && WAVES == 8;
     static constexpr int QROW = DP * 2 + 32;
     static constexpr int LDS = JOIN_LDS + (Q_LDS ? ROWS * QROW : 0);
+    typedef Strays<DT, DP> St;
+    static constexpr int SUFFIX_LDS = LDS + static_cast<int>(sizeof(St));
+    // What the waves tell each other at the end, once for both kinds of shares.
+    struct Ends {
+        float2 ml[WAVES][ROWS];
+        float weight[ROWS][kFinishSplits], own[ROWS], inverse[ROWS];
+    };
+    static __device__ __forceinline__ Ends& ends()
+    {
+        __shared__ Ends e;
+        return e;
+    }
 
     u32x4 k[2][NK], v[NV];
     uint32_t k_scale, v_scale;                                  // of key lane % 32
@@ -265,10 +340,13 @@ struct Few {
     }
 
     // Over the share's keys: sums O, maximum and sum of weights of this wave's tiles.  `page0`: that of key lane % 32 of the first.
+    // SAFE: strays are taken out (see Strays).
+    template <bool SAFE>
     __device__ __forceinline__ void pass(const AttnArgs& a, const Share& s, int32_t page0, char* lds, f32x4 (&o)[DP / 16], float& m, float& l)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+        const int tid = thread<SAFE>(), lane = tid & 63, wave = tid >> 6, g = lane >> 4;
         const Row row = row_of(a, s, lane & 15);
+        if constexpr (SAFE) page0 = s.first + TILE * wave < s.end ? page_of(a, s, s.first + TILE * wave, lane) : 0;
         T8 q[NC];
         const char* const at_q = lds + JOIN_LDS + (lane & 15) * QROW + 16 * g;
         if constexpr (Q_LDS) {
@@ -297,7 +375,8 @@ struct Few {
         while (key0 < s.end) {
             // made anew in every turn, so that what follows from it is not held in registers (from where it would go to scratch memory,
             // whose loads wait for those of keys and values)
-            const int here = thread<Q_LDS>() & 63;
+            int here = lane;
+            if constexpr (Q_LDS) asm volatile("" : "+v"(here));
             clear(a, here);
             // values to LDS, as elements
 #pragma unroll
@@ -344,6 +423,13 @@ struct Few {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (!((mine_there >> (16 * t + r)) & 1) || 16 * t + r > last) z[t][r] = kNone;
+                if (SAFE && now + TILE - 1 > s.sure) {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+                    for (int at = here / (DP / 8); at < TILE; at += 64 / (DP / 8))
+                        if (now + at > s.sure) reinterpret_cast<St*>(lds + LDS)->take_out(mine + at * VROW + 16 * (here % (DP / 8)), now + at, 8 * (here % (DP / 8)));
+                }
             }
             float top = z[0][0];
 #pragma unroll
@@ -377,17 +463,25 @@ struct Few {
         }
     }
 
+    // SUFFIX: there may be keys that not all rows see, and the prefix's parts to join.
+    template <bool SUFFIX>
     __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, int32_t page0, char* lds)
     {
         f32x4 o[NT];
         float m, l;
-        pass(a, s, page0, lds, o, m, l);
+        pass<false>(a, s, page0, lds, o, m, l);
+        const int tid = thread<true>(), lane = tid & 63, wave = tid >> 6, g = lane >> 4;
+        St* const strays = reinterpret_cast<St*>(lds + LDS);
+        bool strayed = false;
+        if (SUFFIX && __builtin_expect(s.sure < kAll, 0)) {     // said to be rare, or the pass above gets fewer registers
+            strayed = strays->template found<WAVES>(o, wave, true);
+            if (__builtin_expect(strayed, 0)) Few().template pass<true>(a, s, 0, lds, o, m, l);
+        }
 
         // the waves' results, joined
-        const int tid = thread<true>(), lane = tid & 63, wave = tid >> 6, g = lane >> 4;
         const Row row = row_of(a, s, lane & 15);
         l = other_half_sum(other_row_sum(l));
-        __shared__ float2 ml[WAVES][ROWS];
+        auto& [ml, weight, own, inverse] = ends();
         if (lane < 16) ml[wave][lane] = make_float2(m, l);
         __syncthreads();
         float best = kNone, sum = 0.0f;
@@ -409,8 +503,8 @@ struct Few {
         }
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
         const float most = best == kNone ? kNone : best * a.c - kLift<DT>;
-        __shared__ float weight[ROWS][kFinishSplits], own[ROWS], inverse[ROWS];
-        if (!a.finish) {
+        const bool finish = SUFFIX && a.finish;
+        if (!finish) {
             if (wave == 0 && lane < 16 && row.in) at_global<float2>(a.part_ml)[s.part * rows + row.global] = make_float2(most, sum);
         } else {
             // the rows' weights of the prefix's parts: a wave takes rows in turn, its lanes the parts
@@ -439,11 +533,15 @@ struct Few {
         for (int i = threadIdx.x; i < ROWS * DP / 4; i += THREADS) {
             const int r = i / (DP / 4), e = 4 * (i % (DP / 4));
             if (r >= s.rows || e >= a.d) continue;
-            const int32_t global = row_of(a, s, r).global;
+            const Row row = row_of(a, s, r);
+            const int32_t global = row.global;
             f32x4 x = *reinterpret_cast<const f32x4*>(join + r * OROW + e);
 #pragma unroll
             for (int w = 1; w < WAVES; ++w) x += *reinterpret_cast<const f32x4*>(join + (w * ROWS + r) * OROW + e);
-            if (!a.finish) {
+            if (SUFFIX && strayed)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] += strays->of(e + j, row.last);
+            if (!finish) {
                 *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + (s.part * rows + global) * a.d + e) = x;
                 continue;
             }
@@ -490,6 +588,8 @@ struct Many {
     static constexpr int KROW = DP * 2 + (WIDE ? 16 : 32), VROW = DP * 2 + (WIDE ? 64 : 32);
     static constexpr int BUF = TILE * (KROW + VROW) + TILE;     // keys, values, a byte for each key that is there
     static constexpr int LDS = 2 * BUF;
+    typedef Strays<DT, DP> St;
+    static constexpr int SUFFIX_LDS = LDS + static_cast<int>(sizeof(St));
     static constexpr bool ONE = DP > 128;                       // one set of pieces on their way
 
     static __device__ __forceinline__ int key_of(int i) { return (THREADS / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
@@ -556,24 +656,34 @@ struct Many {
         }
     };
 
+    // Strays of the pieces that this thread staged.
+    static __device__ __forceinline__ void look_through(const Share& s, int32_t key0, char* buf, char* lds)
+    {
+        const int b = piece() * (CODES ? 2 : 1);
+#pragma unroll 1
+        for (int key = key_of(0); key < TILE; key += THREADS / PIECES)
+            if (key0 + key > s.sure)
+#pragma unroll 1
+                for (int h = 0; h < (CODES ? 2 : 1); ++h) reinterpret_cast<St*>(lds + LDS)->take_out(buf + TILE * KROW + key * VROW + 16 * (b + h), key0 + key, 8 * (b + h));
+    }
+
     static __device__ __forceinline__ A mul(T8 a, T8 b, A c)
     {
         if constexpr (WIDE) return M::template mul32<A>(a, b, c);
         else return M::mul16(a, b, c);
     }
 
-    __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, char* lds)
+    // Over the share's keys: sums O, maximum and sum of weights of this wave's rows and keys of the tiles.
+    template <bool SAFE>
+    __device__ __forceinline__ void pass(const AttnArgs& a, const Share& s, const Row& row, bool busy, char* lds, A (&o)[DP / RW], float& m, float& l)
     {
         // lane = row, and one of 2 (WIDE) or 4 groups of keys or elements
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
-        const int group = wave % GROUPS, part = wave / GROUPS * KEYS;      // its rows, and its keys of a tile
-        const Row row = row_of(a, s, RW * group + r);
-        const bool busy = RW * group < s.rows;                   // waves without rows only help to stage
+        const int part = wave / GROUPS * KEYS;                   // its keys of a tile
         T8 q[NC];
-        A o[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = A{};
-        float m = kNone, l = 0.0f;
+        m = kNone, l = 0.0f;
         const float lag = fminf(kLazy / a.c, kMost);
 
         const auto attend = [&](const char* buf, int32_t key0) {
@@ -668,6 +778,7 @@ struct Many {
             if constexpr (!ONE) ask(odd, s.first + TILE);
             even.clear(a);
             even.stage(lds);
+            if (SAFE && s.first + TILE - 1 > s.sure) look_through(s, s.first, lds, lds);
             if constexpr (ONE) ask(even, s.first + TILE);
             __syncthreads();
             // one turn: `key0`'s tile is in `buf`, the next one arrives in `next`, the one after is asked for into `after`
@@ -677,6 +788,7 @@ struct Many {
                 if (key0 + TILE < s.end) {
                     next.clear(a);
                     next.stage(other);
+                    if (SAFE && key0 + 2 * TILE - 1 > s.sure) look_through(s, key0 + TILE, other, lds);
                 }
                 if constexpr (ONE) ask(after, key0 + 2 * TILE);
                 __syncthreads();
@@ -688,6 +800,25 @@ struct Many {
                 turn(key0 + TILE, lds + BUF, lds, even, second);
             }
             if (key0 < s.end) turn(key0, lds, lds + BUF, second, even);
+        }
+    }
+
+    // SUFFIX: there may be keys that not all rows see, and the prefix's parts to join.
+    template <bool SUFFIX>
+    __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, char* lds)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
+        const int group = wave % GROUPS, part = wave / GROUPS * KEYS;      // its rows, and its keys of a tile
+        const Row row = row_of(a, s, RW * group + r);
+        const bool busy = RW * group < s.rows;                   // waves without rows only help to stage
+        A o[NT];
+        float m, l;
+        pass<false>(a, s, row, busy, lds, o, m, l);
+        St* const strays = reinterpret_cast<St*>(lds + LDS);
+        bool strayed = false;
+        if (SUFFIX && __builtin_expect(s.sure < kAll, 0)) {
+            strayed = strays->template found<WAVES>(o, wave, busy);
+            if (__builtin_expect(strayed, 0)) pass<true>(a, s, row, busy, lds, o, m, l);
         }
         if constexpr (KS == 2) {
             // what the waves of a tile's other half found, register by register
@@ -715,9 +846,14 @@ struct Many {
         if constexpr (!WIDE) l = other_row_sum(l);
         l = other_half_sum(l);
         if (!row.in) return;
+        if (SUFFIX && strayed)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < AN; ++i) o[t][i] += strays->of(RW * t + 8 * (i >> 2) + 4 * g + (i & 3), row.last);
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
         float most = m == kNone ? kNone : m * a.c - kLift<DT>;
-        if (!a.finish) {
+        if (!SUFFIX || !a.finish) {
             const int64_t at = s.part * rows + row.global;
             if (g == 0) at_global<float2>(a.part_ml)[at] = make_float2(most, l);
 #pragma unroll
@@ -781,7 +917,7 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW 
     constexpr int WAVES = threads_of<DP>(PREFIX) / 64;          // few rows use all of them, whatever the prefix's form
     typedef typename form<DT, FORMAT, DP, PREFIX, WAVES>::type P;
     typedef typename form<DT, FORMAT, DP, SUFFIX, WAVES>::type S;
-    __shared__ __attribute__((aligned(16))) char lds[P::LDS > S::LDS ? P::LDS : S::LDS];
+    __shared__ __attribute__((aligned(16))) char lds[P::LDS > S::SUFFIX_LDS ? P::LDS : S::SUFFIX_LDS];
     int32_t b = static_cast<int32_t>(blockIdx.x);
     Share s;
     s.table2 = 0;
@@ -798,9 +934,9 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW 
         s.first = split * a.prefix_chunk;
         s.end = min(s.first + a.prefix_chunk, a.prefix_len);
         s.part = split;
-        s.last0 = kAll;
-        if constexpr (PREFIX == FEW || PREFIX == FEW_8) P().run(a, s, P::page_of(a, s, s.first + P::TILE * (threadIdx.x >> 6), threadIdx.x & 63), lds);
-        else P().run(a, s, lds);
+        s.last0 = s.sure = kAll;
+        if constexpr (PREFIX == FEW || PREFIX == FEW_8) P().template run<false>(a, s, P::page_of(a, s, s.first + P::TILE * (threadIdx.x >> 6), threadIdx.x & 63), lds);
+        else P().template run<false>(a, s, lds);
         return;
     }
     if (threadIdx.x >= S::THREADS) return;                      // a form with more waves than the suffixes' leaves the others idle
@@ -831,13 +967,15 @@ __global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW 
         s.end = a.inline_len ? a.inline_len + keys : min(s.first + a.suffix_chunk, keys);
         s.last0 = a.inline_len + keys - a.q_len;
         if (s.first >= s.end && !a.finish) return;              // the joining kernel knows the length, too
-        S().run(a, s, page0, lds);
+        s.sure = sure_of(a, s);
+        S().template run<true>(a, s, page0, lds);
     } else {
         const int32_t keys = min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), room);
         s.end = min(s.first + a.suffix_chunk, keys);
         s.last0 = keys - a.q_len;
         if (s.first >= s.end && !a.finish) return;
-        S().run(a, s, lds);
+        s.sure = sure_of(a, s);
+        S().template run<true>(a, s, lds);
     }
 }
 
