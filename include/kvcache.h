@@ -35,7 +35,8 @@ enum { KVCACHE_SAME = 0, KVCACHE_E4M3 = 1 };
  *   k, v         device, [tokens, heads, d], last axis contiguous, the others with strides in
  *                elements (host, {token, head})
  *   slots        device, int64 [tokens]; a token whose slot is negative or beyond the cache is
- *                left out; where a slot is named twice, either token may stay
+ *                left out.  A slot is to be named once: where two tokens name one, its place holds
+ *                parts of either, also one's codes with the other's scale, and no other place changes
  *   k_pages ...  device, 16-byte aligned; k_scale, v_scale NULL for KVCACHE_SAME
  * d: a multiple of 16 up to KVCACHE_MAX_HEAD; page_size: a power of two up to 65536.
  * tokens == 0 is a no-op.  Never synchronises, never allocates; can be captured. */

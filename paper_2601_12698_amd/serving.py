@@ -204,7 +204,7 @@ def kvcache_algorithmic_bytes(tokens: int, heads: int, d: int, dtype, quantised:
 
 
 def kvcache_write(k, v, slots, k_pages, v_pages, k_scale, v_scale, dtype, stream=None) -> None:
-    """Tokens k, v [tokens, heads, d] go to their slots (int64 [tokens]) of the pages [pages, heads, page_size, d]: quantised
+    """Tokens k, v [tokens, heads, d] go to their slots (int64 [tokens], each named once) of the pages [pages, heads, page_size, d]: quantised
     where the pages are ``float8_e4m3fn`` (or bytes) with scale bytes [pages, heads, page_size], else copied (scales None)."""
     if stream is None and (B._torch_facts or B._torch()) and (native := _fast()) is not None:
         st = native.kvcache_write(k, v, slots, k_pages, v_pages, k_scale, v_scale, dtype)
