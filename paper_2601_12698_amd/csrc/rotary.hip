@@ -27,14 +27,20 @@ struct RotaryArgs {
     int32_t q_heads, heads, pairs, pair_pieces, pieces, axes, tokens_per_wg, heads_per_wg, sign;
 };
 
-// cos and sin of 2 pi r, r in fp64.  The eighth of a turn that is left after the nearest quarter is taken off is at most
-// pi/4 = 0.785 and goes through the series of sine and cosine in fp32, cut after x^9 and x^10: what is left out is
-// x^11 / 11! = 1.8e-9 and x^12 / 12! = 1.2e-10, a thirtieth of an fp32 half step.
-__device__ __forceinline__ float2 turn_of(double r)
+// cos and sin of an angle in fp64, within 2 units in the last place of fp32.  Where the angle is near a whole number of quarter turns
+// its sine or cosine is what remains after they are taken off, so 1 / (2 pi) is two numbers here and the product's rounding is kept: of
+// an angle of a million one number leaves 10^-10, and the sine near a half turn, 1e-6 say, would have three digits too few.  What
+// remains is at most an eighth of a turn, pi/4 = 0.785, and goes through the series of sine and cosine in fp32, cut after x^9 and x^10:
+// what is left out is x^11 / 11! = 1.8e-9 and x^12 / 12! = 1.2e-10, a seventeenth of an fp32 half step at 0.707, and less.
+__device__ __forceinline__ float2 turn_of(double angle)
 {
+    constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;        // 1 / (2 pi)
+    const double r = angle * kTurn, rest = __builtin_fma(angle, kTurnRest, __builtin_fma(angle, kTurn, -r));
     const double quarters = r * 4.0, whole = __builtin_rint(quarters);
-    const float x = static_cast<float>((quarters - whole) * 1.57079632679489661923);
-    const int which = static_cast<int>(whole - 4.0 * __builtin_floor(whole * 0.25));          // 0..3
+    const double near = __builtin_fma(4.0, rest, quarters - whole), more = __builtin_rint(near);   // more: 0 below 2^50 quarters, but for borders
+    const float x = static_cast<float>((near - more) * 1.57079632679489661923);
+    const double turns = whole - 4.0 * __builtin_floor(whole * 0.25) + more;
+    const int which = static_cast<int>(turns - 4.0 * __builtin_floor(turns * 0.25));          // 0..3
     const float y = x * x;
     const float s = __builtin_fmaf(
         x * y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -1.66666667e-1f), x);
@@ -102,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
                 const int32_t token = i / a.pairs, pair = i - token * a.pairs;
                 const int32_t axis = min(static_cast<int32_t>(at_global<const uint8_t>(a.pair_axis)[pair]), a.axes - 1);
                 const double angle = static_cast<double>(pos[axis * a.tokens + t0 + token]) * at_global<const double>(a.inv_freq)[pair];
-                float2 cs = turn_of(angle * 0.15915494309189533577);
+                float2 cs = turn_of(angle);
                 if (a.sign < 0) cs.y = -cs.y;
                 turns[i] = cs;
             }
