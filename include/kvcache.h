@@ -6,7 +6,8 @@
  * a page lie one behind the other.  A token's place is its slot: page * page_size + offset.
  *   KVCACHE_SAME   elements of the activations' type (ADDRMS_BF16 or ADDRMS_FP16), copied
  *   KVCACHE_E4M3   one byte an element (OCP e4m3) and one scale byte s for each token and head,
- *                  k_scale and v_scale [pages][heads][page_size]; the value is code * 2^(s - 127), s from 1 to 254
+ *                  k_scale and v_scale [pages][heads][page_size]; the value is code * 2^(s - 127).  A write
+ *                  gives s from 1 to 254; 0 is 2^-127 to those who read, and 255 makes the row NaN
  *
  * Quantisation of a row x of d elements: a = max |x|; e = the least whole number with
  * a * 2^-e <= 448 (448 is the format's largest value), at least -126 and at most 127, and 0 for a

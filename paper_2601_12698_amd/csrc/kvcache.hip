@@ -140,7 +140,8 @@ struct Piece {
         typedef typename elem<DT>::type T;
         if constexpr (FORMAT != KVCACHE_E4M3) return same;
         vec8<DT> x;
-        const float by = scale ? __builtin_bit_cast(float, scale << 23) : 0x1p-127f;
+        // the exponent; with the fraction's first bit, 0 is 2^-127 and 255 NaN
+        const float by = __builtin_bit_cast(float, scale << 23 | (scale - 1 >= 254 ? 0x400000u : 0u));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes[j]), false);

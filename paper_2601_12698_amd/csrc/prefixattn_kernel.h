@@ -66,6 +66,7 @@ template <int DT> constexpr float kLift = DT == DT_FP16 ? 7.0f : 0.0f;
 constexpr uint64_t full_of(int bits) { return bits == 64 ? ~0ull : (1ull << bits) - 1; }
 constexpr float kNone = -__builtin_huge_valf();
 
+// A row's scale as the conversions take it: they look at the exponent alone, to which 0 is 2^-127 and 255 NaN.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // Eight codes as elements, times their row's power of two.
