@@ -39,7 +39,8 @@ enum { KVCACHE_SAME = 0, KVCACHE_E4M3 = 1 };
  *                left out.  A slot is to be named once: where two tokens name one, its place holds
  *                parts of either, also one's codes with the other's scale, and no other place changes
  *   k_pages ...  device, 16-byte aligned; k_scale, v_scale NULL for KVCACHE_SAME
- * d: a multiple of 16 up to KVCACHE_MAX_HEAD; page_size: a power of two up to 65536.
+ * d: a multiple of 16 up to KVCACHE_MAX_HEAD; page_size: a power of two up to 65536; heads up to 65536; pages
+ * below 2^31; tokens * heads * (d / 8, up to a power of two) below 2^32, and tokens * heads below 2^31.
  * tokens == 0 is a no-op.  Never synchronises, never allocates; can be captured. */
 int kvcache_write(const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides,
                   const int64_t* slots, void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale,

@@ -178,6 +178,14 @@ __global__ __launch_bounds__(kThreads) void read_kernel(CacheArgs a)
     put<PAST>(reinterpret_cast<vec8<DT>*>(at_global<T>(a.v) + row * a.d + 8 * lane), v);
 }
 
+// Workgroups of a launch; a write goes by blocks of tokens.
+int64_t groups_of(int64_t tokens, int32_t heads, int32_t d)
+{
+    const int64_t per = kThreads >> log2_of(d / 8);
+    return (tokens * heads + per - 1) / per;
+}
+int64_t whole_blocks(int64_t tokens) { return (tokens + kBlock - 1) / kBlock * kBlock; }
+
 int check(int64_t tokens, int32_t heads, int32_t d, int64_t pages, int32_t page_size, int dtype, int format)
 {
     if (dtype != ADDRMS_BF16 && dtype != ADDRMS_FP16) return fail(ADDRMS_ERR_UNSUPPORTED_DTYPE, "unsupported dtype %d for a cache", dtype);
@@ -186,7 +194,7 @@ int check(int64_t tokens, int32_t heads, int32_t d, int64_t pages, int32_t page_
     if (!power_of_two(page_size) || page_size > 65536) return fail(ADDRMS_ERR_INVALID_ARG, "page_size must be a power of two up to 65536 (got %d)", page_size);
     if (d % 16 != 0 || d > KVCACHE_MAX_HEAD)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "d=%d is not a multiple of 16 up to %d", d, KVCACHE_MAX_HEAD);
-    if (heads > 65536 || pages >= (1ll << 31) || tokens >= (1ll << 31) / heads - kBlock)
+    if (heads > 65536 || pages >= (1ll << 31) || tokens >= (1ll << 31) / heads - kBlock || !launchable(groups_of(whole_blocks(tokens), heads, d), kThreads))
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld tokens of %d heads or %lld pages are beyond the limits", (long long)tokens, heads, (long long)pages);
     return ADDRMS_OK;
 }
@@ -201,11 +209,6 @@ CacheArgs args_of(const int64_t* slots, int64_t tokens, int32_t heads, int32_t d
     a.heads = static_cast<uint32_t>(heads), a.d = static_cast<uint32_t>(d);
     a.page_shift = static_cast<uint32_t>(log2_of(page_size)), a.lanes_log2 = static_cast<uint32_t>(log2_of(d / 8));
     return a;
-}
-unsigned grid_of(const CacheArgs& a, int64_t tokens)
-{
-    const int64_t per = kThreads >> a.lanes_log2;
-    return static_cast<unsigned>((tokens * a.heads + per - 1) / per);
 }
 
 }  // namespace
@@ -230,7 +233,7 @@ int kvcache_write(const void* k, const int64_t* k_strides, const void* v, const 
         bits |= static_cast<uint64_t>(a.ks[i] | a.vs[i]) * 2;
     }
     const bool wide = bits % 16 == 0;        // else element by element
-    const dim3 grid(grid_of(a, (tokens + kBlock - 1) / kBlock * kBlock));
+    const dim3 grid(static_cast<unsigned>(groups_of(whole_blocks(tokens), heads, d)));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool past = a.rows * d * 4 >= kPastBytes;
 #define GO(DT, F) launch_kernel(!wide ? write_kernel<DT, F, false, false> : past ? write_kernel<DT, F, true, true> : write_kernel<DT, F, true, false>, grid, kThreads, s, a)
@@ -250,7 +253,7 @@ int kvcache_read(const void* k_pages, const void* v_pages, const uint8_t* k_scal
         return fail(ADDRMS_ERR_MISALIGNED, "pages and outputs must be 16-byte aligned and slots 8-byte");
     CacheArgs a = args_of(slots, tokens, heads, d, pages, page_size);
     a.k = addr(k_out), a.v = addr(v_out), a.k_pages = addr(k_pages), a.v_pages = addr(v_pages), a.k_scale = addr(k_scale), a.v_scale = addr(v_scale);
-    const dim3 grid(grid_of(a, tokens));
+    const dim3 grid(static_cast<unsigned>(groups_of(tokens, heads, d)));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool past = a.rows * d * 4 >= kPastBytes;
 #define GO(DT, F) launch_kernel(past ? read_kernel<DT, F, true> : read_kernel<DT, F, false>, grid, kThreads, s, a)

@@ -71,6 +71,9 @@ inline int log2_of(int64_t n)
     return s;
 }
 
+// A launch numbers its threads along an axis in 32 bits.
+inline bool launchable(int64_t groups, int64_t threads) { return groups * threads < (1ll << 32); }
+
 // A launch whose status is its own: an error that other code of the process left behind is not taken for it.
 template <typename Args>
 hipError_t launch_kernel(void (*kernel)(Args), dim3 grid, dim3 block, hipStream_t stream, const Args& args)
