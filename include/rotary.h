@@ -36,7 +36,8 @@ enum { ROTARY_INTERLEAVED = 1, ROTARY_INVERSE = 2 };
  *   positions    device, int64 [axes][tokens]
  *   inv_freq     device, fp64 [rot / 2], radians a position
  *   pair_axis    device, uint8 [rot / 2], below axes (a larger number counts as axes - 1)
- * rot is even, 2 <= rot <= d <= ROTARY_MAX_HEAD; 1 <= axes <= 255.  tokens == 0 is a no-op.
+ * rot is even, 2 <= rot <= d <= ROTARY_MAX_HEAD; 1 <= axes <= 255; q_heads + k_heads up to 65536; tokens below
+ * 2^31, and of more than tokens * d = 2^32 some calls are refused.  tokens == 0 is a no-op.
  * Never synchronises, never allocates; can be captured into a HIP graph. */
 int rotary_run(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides,
                void* q_out, const int64_t* q_out_strides, void* k_out, const int64_t* k_out_strides,

@@ -223,6 +223,7 @@ int rotary_run(const void* q, const int64_t* q_strides, const void* k, const int
     a.heads_per_wg = a.heads;
     const int64_t groups = (tokens + per - 1) / per;
     if (groups < many && a.heads > iy) a.heads_per_wg = iy;
+    if (!launchable(groups, ix)) return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld tokens of d=%d are too many for a launch", (long long)tokens, d);
     const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((a.heads + a.heads_per_wg - 1) / a.heads_per_wg)), block(ix, iy);
     // Outputs that the L2s would not keep for the next kernel go past them where every store fills its 16-byte pieces' lines (8191
     // tokens x 40 heads x 128 bf16 38.5 -> 32.5 us, 2048 x 40 x 96 fp32 13.9 -> 11.3, 1000 x 40 x 128 bf16 6.8 -> 5.8; 200 tokens, 2 MB,

@@ -6,7 +6,7 @@ import pytest
 
 from paper_2601_12698_amd import binding as B
 from paper_2601_12698_amd import serving as S
-from test_serving_checks import cache_read, cache_write
+from test_serving_checks import cache_read, cache_write, rotary
 
 
 @pytest.mark.parametrize("call", [cache_write, cache_read])
@@ -20,3 +20,26 @@ def test_a_cache_call_has_fewer_than_2_to_32_threads(call, heads, d, lanes):
             assert call(tokens=tokens, heads=heads, d=d, ks=st, vs=st) == B.ERR_UNSUPPORTED_SHAPE, tokens
     fits = most - 300                                          # of whole workgroups of 256 threads
     assert S.load().kvcache_algorithmic_bytes(fits, heads, d, 0, 1) == 2 * fits * heads * (3 * d + 1) + 8 * fits
+
+
+def test_rotary_calls_beyond_a_launch():
+    """Heads of 256 elements that are not aligned, two of them turned: 255 threads a head, two tokens a workgroup."""
+    st = (c_int64 * 2)(257, 257)
+    one = dict(qs=st, qos=st, hq=1, hk=0, d=256, rot=2, axes=1, dtype=0)
+    for tokens in (2 * ((1 << 32) // 255) + 2, (1 << 30) + 1, (1 << 31) - 1):
+        assert rotary(tokens=tokens, **one) == B.ERR_UNSUPPORTED_SHAPE, tokens
+
+
+@pytest.mark.gpu
+def test_rotary_with_as_many_heads_as_a_call_takes():
+    """65536 heads, one a workgroup: as many workgroups along an axis."""
+    import torch
+
+    import serving_ref as R
+    x = torch.randn(1, 65536, 257, generator=torch.Generator().manual_seed(1)).to(torch.float16)[:, :, :256]
+    out = torch.zeros(1, 65536, 257, dtype=torch.float16, device="cuda")[:, :, :256]
+    dev = torch.zeros(1, 65536, 257, dtype=torch.float16, device="cuda")[:, :, :256].copy_(x)
+    pos, freq, axis = torch.tensor([[5]]), torch.ones(1, dtype=torch.float64), torch.zeros(1, dtype=torch.uint8)
+    S.rotary_run(dev[:, :65535], dev[:, 65535:], out[:, :65535], out[:, 65535:], pos.cuda(), freq.cuda(), axis.cuda(), "fp16")
+    want = R.rotary(x, pos, freq, axis)
+    assert ((out.cpu().double() - want).abs() <= 2.0 ** -11 * want.abs() + 2.0 ** -20 * (1 + x.double().abs().amax())).all()
