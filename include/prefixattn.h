@@ -30,8 +30,8 @@ extern "C" {
 /* Sizes of a call: host. */
 typedef struct prefixattn_shape {
     int32_t batch;          /* sequences                                                   */
-    int32_t q_len;          /* queries of each                                             */
-    int32_t q_heads;        /* a multiple of kv_heads                                      */
+    int32_t q_len;          /* queries of each; batch * q_len * q_heads up to 2^24         */
+    int32_t q_heads;        /* a multiple of kv_heads, up to 65536                         */
     int32_t kv_heads;
     int32_t d;              /* a multiple of 16 up to KVCACHE_MAX_HEAD                     */
     int32_t page_size;      /* a power of two up to 65536                                  */

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a)
     }
 }
 
-constexpr int64_t kMaxBlocks = 1 << 24;      // of 256 threads: a launch has fewer than 2^32
+constexpr int64_t kMaxRows = 1 << 24;        // queries by heads: their numbers, and those of what is formed of them, are 32 bits
 // The shortest piece of keys; of a suffix as long as the prefix's, up to twice this.  128 beside 256, whole calls: 8 x 40 heads over
 // 2000 bf16 keys 12.8 and 14.2 us, 2 x 40 over 900 e4m3 10.8 and 11.2, 8 x 40 over 8191 the same; a long prefix with the suffixes in
 // pieces of 128 has too little room left: 4 x 32 heads over 131072 bf16 keys and suffixes of 2000 112 us, with pieces of 256 103.5.
@@ -128,6 +128,14 @@ struct Plan {
     int64_t rows, prefix_blocks, suffix_blocks, bytes;
     bool finish;                             // the suffixes' workgroups are a launch of their own that joins the prefix's parts
 };
+
+// Whether launches hold a plan's workgroups.
+int fits(const Plan& p)
+{
+    const int64_t beside = p.prefix_blocks + (p.finish ? 0 : p.suffix_blocks);
+    if (launchable(beside, threads_of(p.prefix_form, p.dp)) && launchable(p.suffix_blocks, threads_of(p.suffix_form, p.dp))) return ADDRMS_OK;
+    return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)(p.prefix_blocks + p.suffix_blocks));
+}
 
 // Checks a shape and splits its work.  A key range is split until there are as many workgroups as `wanted` says,
 // in pieces of kMinChunk keys or more; what a suffix may hold at most counts, for its length is known on the device alone.
@@ -159,7 +167,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     p->dp = s->d <= 64 ? 64 : s->d <= 128 ? 128 : 256;
     if (s->batch == 0 || s->q_len == 0) return ADDRMS_OK;
     const int64_t tokens = static_cast<int64_t>(s->batch) * s->q_len;
-    if (tokens > kMaxBlocks || tokens * s->q_heads > kMaxBlocks)
+    if (tokens > kMaxRows || tokens * s->q_heads > kMaxRows)
         return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld queries of %d heads are beyond the limit (2^24 together)", (long long)tokens, s->q_heads);
     p->rows = tokens * s->q_heads;
     const int64_t all = tokens * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
@@ -194,7 +202,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         a.suffix_tiles = a.suffix_splits = 1;
         a.suffix_chunk = static_cast<int32_t>(width);
         p->suffix_blocks = units;
-        return p->suffix_blocks > kMaxBlocks ? fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)p->suffix_blocks) : ADDRMS_OK;
+        return fits(*p);
     }
     const bool prefix = a.prefix_len && a.pages, suffix = width && a.pages;
     if (!prefix) p->prefix_form = p->suffix_form;
@@ -224,10 +232,8 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     }
     p->prefix_blocks = (static_cast<int64_t>(a.prefix_splits) * a.kv_heads + 7) / 8 * 8 * a.prefix_tiles;
     const int64_t parts = a.prefix_splits + (p->finish ? 0 : a.suffix_splits);
-    if (p->prefix_blocks + p->suffix_blocks > kMaxBlocks)
-        return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)(p->prefix_blocks + p->suffix_blocks));
     p->bytes = parts * p->rows * (4ll * a.d + 8);
-    return ADDRMS_OK;
+    return fits(*p);
 }
 
 }  // namespace

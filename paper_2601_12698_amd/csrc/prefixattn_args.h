@@ -23,6 +23,8 @@ struct AttnArgs {
 // Forms of a workgroup: 16 rows whose four (FEW_8: eight) waves take keys in turn; 64, 128 or 256 rows that share their keys (64:
 // heads up to 128; 256: heads of 65 to 128).
 enum : int { FEW = 0, MANY_64 = 1, MANY_128 = 2, MANY_256 = 3, FEW_8 = 4 };
+// Threads of a workgroup; heads over 128 leave no registers for two of 128 rows on a CU.
+constexpr int threads_of(int form, int padded_head) { return form == FEW_8 || form == MANY_256 || (form == MANY_128 && padded_head > 128) ? 512 : 256; }
 constexpr int kJoinThreads = 256;
 constexpr int kFormRows[] = {16, 64, 128, 256, 16};
 constexpr int kChunkStep = 128;                       // splits begin at multiples of this many keys: every tile is aligned

@@ -904,7 +904,6 @@ struct Many {
 // Workgroups of the prefix first, then those of the suffixes.  Workgroups go round the 8 XCDs; the row tiles of one head and
 // key range stand 8 apart, so that they read it through the same L2 at the same time.
 // FORM: see prefixattn_args.h.
-template <int DP> constexpr int threads_of(int form) { return form == FEW_8 || form == MANY_256 || (form == MANY_128 && DP > 128) ? 512 : 256; }
 template <int DT, int FORMAT, int DP, int FORM, int WAVES> struct form;
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW, WAVES> { typedef Few<DT, FORMAT, DP, WAVES> type; };
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, FEW_8, WAVES> { typedef Few<DT, FORMAT, DP, 8> type; };
@@ -913,9 +912,9 @@ template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MAN
 template <int DT, int FORMAT, int DP, int WAVES> struct form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8> type; };
 
 template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX>
-__global__ __launch_bounds__(threads_of<DP>(PREFIX), (DP > 128 && PREFIX == FEW ? 1 : 2)) void attn_kernel(AttnArgs a)
+__global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW ? 1 : 2)) void attn_kernel(AttnArgs a)
 {
-    constexpr int WAVES = threads_of<DP>(PREFIX) / 64;          // few rows use all of them, whatever the prefix's form
+    constexpr int WAVES = threads_of(PREFIX, DP) / 64;          // few rows use all of them, whatever the prefix's form
     typedef typename form<DT, FORMAT, DP, PREFIX, WAVES>::type P;
     typedef typename form<DT, FORMAT, DP, SUFFIX, WAVES>::type S;
     __shared__ __attribute__((aligned(16))) char lds[P::LDS > S::SUFFIX_LDS ? P::LDS : S::SUFFIX_LDS];

@@ -7,7 +7,7 @@ namespace {
 template <int PREFIX, int SUFFIX>
 hipError_t launch(const AttnArgs& a, unsigned blocks, hipStream_t s)
 {
-    return launch_kernel(attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX, SUFFIX>, dim3(blocks), dim3(threads_of<UNIT_DP>(PREFIX)), s, a);
+    return launch_kernel(attn_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX, SUFFIX>, dim3(blocks), dim3(threads_of(PREFIX, UNIT_DP)), s, a);
 }
 
 }  // namespace

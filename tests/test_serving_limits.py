@@ -1,12 +1,12 @@
 """The largest sizes that the operators around a decode step's attention take: a call beyond them is refused for its shape before anything is
 launched, not by the launch.  (On the CPU; what is within them is asked of functions that launch nothing.)"""
-from ctypes import c_int64
+from ctypes import byref, c_int64
 
 import pytest
 
 from paper_2601_12698_amd import binding as B
 from paper_2601_12698_amd import serving as S
-from test_serving_checks import cache_read, cache_write, rotary
+from test_serving_checks import attend, cache_read, cache_write, rotary, shape
 
 
 @pytest.mark.parametrize("call", [cache_write, cache_read])
@@ -28,6 +28,19 @@ def test_rotary_calls_beyond_a_launch():
     one = dict(qs=st, qos=st, hq=1, hk=0, d=256, rot=2, axes=1, dtype=0)
     for tokens in (2 * ((1 << 32) // 255) + 2, (1 << 30) + 1, (1 << 31) - 1):
         assert rotary(tokens=tokens, **one) == B.ERR_UNSUPPORTED_SHAPE, tokens
+
+
+def test_attention_calls_beyond_a_launch():
+    """2^24 sequences of one head: a workgroup of 256 threads each, 2^32 together, one too many.  One sequence fewer is planned."""
+    few = dict(q_heads=1, kv_heads=1, d=64, prefix_len=0, suffix_width=1)
+    assert S.prefixattn_workspace_bytes(shape(batch=(1 << 24) - 1, **few)) == 0
+    s = shape(batch=1 << 24, **few)
+    assert S.load().prefixattn_workspace_bytes(byref(s)) == B.ERR_UNSUPPORTED_SHAPE and attend(s) == B.ERR_UNSUPPORTED_SHAPE
+    for more in (dict(batch=(1 << 24) + 1), dict(batch=1 << 20, q_len=17)):
+        assert attend(shape(**{**few, **more})) == B.ERR_UNSUPPORTED_SHAPE
+    # as many rows in workgroups that have 64 and more
+    assert S.prefixattn_workspace_bytes(shape(batch=1, q_len=1 << 24, **few)) >= 0
+    assert S.prefixattn_workspace_bytes(shape(batch=1 << 17, q_len=128, **few)) >= 0
 
 
 @pytest.mark.gpu
