@@ -55,7 +55,7 @@ int64_t prefixattn_workspace_bytes(const prefixattn_shape* shape);
  *                 A page number outside the cache is a page of masked keys.
  *   out           device, [batch * q_len, q_heads, d], contiguous, 16-byte aligned; must not overlap q
  *   lse           device, fp32 [batch * q_len, q_heads], or NULL
- *   scale         > 0, finite
+ *   scale         > 0, and finite times log2(e): up to 2.35e38
  *   workspace     device, 16-byte aligned, workspace_bytes >= prefixattn_workspace_bytes(shape); not for two
  *                 calls at a time, free again when the call's work is done
  * batch == 0 or q_len == 0 is a no-op.  Never synchronises, never allocates; can be captured into a HIP graph: page

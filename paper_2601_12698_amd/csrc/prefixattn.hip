@@ -262,7 +262,8 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
 {
     Plan p;
     if (const int st = plan_of(shape, &p)) return st;
-    if (!(scale > 0.0f) || !(scale < INFINITY)) return fail(ADDRMS_ERR_INVALID_ARG, "scale must be > 0 and finite (got %g)", static_cast<double>(scale));
+    const float c = scale * 1.44269504088896340736f;
+    if (!(scale > 0.0f) || !(c < INFINITY)) return fail(ADDRMS_ERR_INVALID_ARG, "scale must be > 0, and finite times log2(e) (got %g)", static_cast<double>(scale));
     if (shape->batch == 0 || shape->q_len == 0) return ADDRMS_OK;
     AttnArgs& a = p.a;
     const bool codes = shape->format == KVCACHE_E4M3, keys = a.prefix_splits || a.suffix_splits, own = a.suffix_splits && shape->suffix_width;
@@ -280,7 +281,7 @@ int prefixattn_run(const void* q, const int64_t* q_strides, const void* k_pages,
     a.part_ml = a.part_o + 4ull * (p.bytes / (4ll * a.d + 8)) * a.d;
     a.q_token = q_strides[0], a.q_head = q_strides[1];
     a.q_wide = (a.q | static_cast<uint64_t>(q_strides[0] * 2) | static_cast<uint64_t>(q_strides[1] * 2)) % 16 == 0;
-    a.c = scale * 1.44269504088896340736f;
+    a.c = c;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     static constexpr AttnLaunch kUnits[2][2][3] = {
         {{ATTN_UNIT(0, 0, 64), ATTN_UNIT(0, 0, 128), ATTN_UNIT(0, 0, 256)}, {ATTN_UNIT(0, 1, 64), ATTN_UNIT(0, 1, 128), ATTN_UNIT(0, 1, 256)}},

@@ -43,6 +43,24 @@ def test_attention_calls_beyond_a_launch():
     assert S.prefixattn_workspace_bytes(shape(batch=1 << 17, q_len=128, **few)) >= 0
 
 
+def test_a_scale_whose_product_with_log2_e_is_no_number_is_refused():
+    """Scores are formed as powers of two; beyond this scale every weight would be NaN, also where scores are small."""
+    for scale in (2.36e38, 3e38, 3.4e38):
+        assert attend(shape(), scale=scale) == B.ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("q_len", [1, 20])
+def test_a_huge_scale(q_len):
+    """Tiny queries and a scale to match: as their product would be."""
+    import torch
+
+    from test_gpu_prefixattn import build, call, check
+    c, dtype = build((1, q_len, 4, 1, 64, 30, [q_len], 2, 16, "bf16", False), seed=1)
+    c["q"], c["scale"] = (c["q"].double() * 2.0 ** -115).to(torch.bfloat16), 2.0 ** 112
+    check(c, dtype, call(c, dtype))
+
+
 @pytest.mark.gpu
 def test_rotary_with_as_many_heads_as_a_call_takes():
     """65536 heads, one a workgroup: as many workgroups along an axis."""
