@@ -123,7 +123,7 @@ class Layer:
 def run(batch=8, prompt=1000, steps=16, cache="e4m3", check=False, graph=True):
     layer = Layer(batch, prompt, steps + 1, cache)
     layer.prefill()
-    layer.step()
+    q = layer.step()
     side = torch.cuda.Stream()
     torch.cuda.synchronize()
     if graph and steps > 2:
@@ -157,6 +157,8 @@ def main():
     ap.add_argument("--cache", choices=("e4m3", "same"), default="e4m3")
     ap.add_argument("--check", action="store_true")
     a = ap.parse_args()
+    if a.batch < 1 or a.prompt < 1 or a.steps < 1:
+        ap.error("--batch, --prompt and --steps must be at least 1")
     layer, us, error = run(a.batch, a.prompt, a.steps, a.cache, a.check)
     print(f"{a.batch} sequences over a prompt of {a.prompt}: {int(layer.suffix_lens[0])} tokens each"
           + (f", {us:.1f} us a step" if us else "") + (f", attention {error:.1e} from plain torch" if error is not None else ""))
