@@ -156,7 +156,8 @@ hipError_t launch(const RotaryArgs& a, bool inter, bool past, dim3 grid, dim3 bl
     return launch_kernel(past ? rotary_kernel<DT, V, false, true> : rotary_kernel<DT, V, false, false>, grid, block, s, a);
 }
 
-// True if the bytes that [tokens, heads, d] with these strides spans hold two elements at one place.
+// False where [tokens, heads, d] with these strides may put two elements at one place.  (True only where one axis's steps enclose
+// the other axis whole; strides that interleave without meeting are taken for such that meet.)
 bool strides_fit(const int64_t* st, int64_t tokens, int64_t heads, int64_t d)
 {
     const int64_t a = st[0] < 0 ? -st[0] : st[0], b = st[1] < 0 ? -st[1] : st[1];
