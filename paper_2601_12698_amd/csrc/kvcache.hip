@@ -5,9 +5,11 @@
 // A row is 2 to 32 neighbouring lanes of 8 elements each, keys and values together.  A row that is written stays in registers: its
 // lanes find the largest magnitude by exchanges and then round.  (A lane of 16 elements loads 16 bytes of codes at once, but then
 // its two stores of 16 bytes each fill every other half line: 131072 tokens x 8 x 128 bf16 165 us, with 8 elements 146.)
-// Results beyond an L2 go past the caches: 131072 tokens read back 146 -> 138 us, 16384 22.5 -> 17.3 (5.8 TB/s), 4999 x 4 x 256 fp16
-// 6.5 -> 6.4; written, 16384 x 8 x 128 23.2 -> 20.2 us, 4999 x 4 x 256 8.5 -> 7.9, 131072 151 -> 148; 64 tokens 2.7 either way.
-// Loads that go past them lose 2 to 20 %.
+// Results of 4 MB and more (keys and values in 16 bits) go past the caches: 131072 tokens read back 146 -> 138 us, 16384 22.5 -> 17.3
+// (5.8 TB/s), 4999 x 4 x 256 fp16 6.5 -> 6.4; written, 16384 x 8 x 128 23.2 -> 20.2 us, 4999 x 4 x 256 8.5 -> 7.9, 131072 151 -> 148; 512
+// to 2048 tokens the same.  What comes next reads them from memory: a write of 131072 tokens and attention of 4 x 32 heads to them 192
+// us, not 199, of 16384 33.6 and 33.1; 16384 read back and copied 42.4 and 37.3, 131072 339 and 334, 8192 and two matrix products
+// 46.5 and 45.4, 2048 41.0 and 41.2.  Loads that go past the caches lose 2 to 20 %.
 #include "kvcache.h"
 #include "serving_internal.h"
 
@@ -18,7 +20,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr uint32_t kBlock = 8;               // tokens of a head that are written side by side (16384 x 8 x 128: 21.4 us token by token, 19.8 with 8 or 16)
-constexpr int64_t kPastBytes = 4 << 20;      // of keys and values in 16 bits: the L2 of one XCD
+constexpr int64_t kPastBytes = 4 << 20;      // of keys and values in 16 bits
 
 struct CacheArgs {
     addr_t k, v, slots, k_pages, v_pages, k_scale, v_scale;

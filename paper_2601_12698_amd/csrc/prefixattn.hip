@@ -173,7 +173,9 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     const int64_t all = tokens * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
     // The least form that has the rows (with 64 rows in 128: 16 x 32 heads over 16384 keys, bf16 25.4 us and 26.0, e4m3 22.2 and 24.0).
     // Heads over 128 go from 16 to 128: with 16 rows a wave, a form for 64 took 53 us in place of 41 for 20 rows over 16384 bf16 keys
-    // of 256, 54 and 53 for 32, 63 and 59 for 64 (in e4m3 36.5 and 41).
+    // of 256, 54 and 53 for 32, 63 and 59 for 64 (in e4m3 36.5 and 41).  Heads up to 64 end with 128 rows: a tile of e4m3 keys has fewer
+    // pieces of 16 bytes than 512 threads, and in 16 bits a form for 256 rows takes 67.2 us in place of 72.1 for 64 x 64 heads over 32768
+    // keys, but 48.0 in place of 41.2 for 8 x 64 queries of 32 heads over 4096 and 46.1 in place of 39.3 for 2 x 512 over 1000.
     auto form_of = [p](int64_t rows) { return rows <= 16 ? FEW : rows <= 64 && p->dp <= 128 ? MANY_64 : rows <= 128 || p->dp != 128 ? MANY_128 : MANY_256; };
     auto tiles = [](int64_t rows, int form) { return (rows + kFormRows[form] - 1) / kFormRows[form]; };
     p->suffix_form = form_of(own);
@@ -220,9 +222,10 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         // One launch for both: the prefix leaves the suffixes their places, up to half of all.  Where a workgroup's own pace is the bound
         // (not with few rows, where memory is), only if its pieces grow by no more keys than a suffix's piece has, and as many as its
         // start takes the time of (about kMinChunk), for it else runs behind them: 16 x 4 queries over 4001 fp16 keys of 256 and
-        // suffixes of 300 take 53.6 us with them behind, 42 beside; 8 x 40 heads over 8191 e4m3 keys and one page 19.9 behind, 16.2
-        // beside; over 131072 and suffixes of 500 69 behind, 87 beside; with few rows, 4 x 32 heads over 131072 bf16 keys and
-        // suffixes of 2000, 106 behind, 103 beside.
+        // suffixes of 300 take 43.9 us with them behind, 38.2 beside, of one page 37.8 and 37.0; 8 x 40 heads over 8191 e4m3 keys and one
+        // page 19.9 behind, 15.9 beside; over 131072 and suffixes of 500 70.6 behind, 80.5 beside; 4 x 16 queries of 32 heads over 20000
+        // bf16 keys and suffixes of 1000 53.0 behind, 54.7 beside; with few rows, 4 x 32 heads over 131072 bf16 keys and suffixes of 2000,
+        // 103.0 behind, 101.8 beside.
         if (!p->finish && prefix) {
             const int32_t splits = a.prefix_splits, chunk = a.prefix_chunk;
             split_prefix(std::max(slots / 2, slots - p->suffix_blocks));

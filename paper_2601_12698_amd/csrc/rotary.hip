@@ -18,7 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTurns = 2048;              // angles of one workgroup: 16 KiB of LDS
 constexpr int kAhead = 2;                    // pieces of a thread that are under way together (8191 x 40 x 128 bf16: 2 38.5 us, 4 42.5, 8 48)
-constexpr int64_t kPastBytes = 4 << 20;      // of output: the L2 of one XCD
+constexpr int64_t kPastBytes = 4 << 20;      // of output (see rotary_run)
 
 struct RotaryArgs {
     addr_t q, k, q_out, k_out, positions, inv_freq, pair_axis;
@@ -226,9 +226,11 @@ int rotary_run(const void* q, const int64_t* q_strides, const void* k, const int
     if (groups < many && a.heads > iy) a.heads_per_wg = iy;
     if (!launchable(groups, ix)) return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "%lld tokens of d=%d are too many for a launch", (long long)tokens, d);
     const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((a.heads + a.heads_per_wg - 1) / a.heads_per_wg)), block(ix, iy);
-    // Outputs that the L2s would not keep for the next kernel go past them where every store fills its 16-byte pieces' lines (8191
-    // tokens x 40 heads x 128 bf16 38.5 -> 32.5 us, 2048 x 40 x 96 fp32 13.9 -> 11.3, 1000 x 40 x 128 bf16 6.8 -> 5.8; 200 tokens, 2 MB,
-    // 3.6 either way).  Loads that go past them, too, gain 2 % at the largest and lose a quarter at the others.
+    // Large outputs go past the caches where every store fills its 16-byte pieces' lines: 8192 tokens x 40 heads x 128 bf16 26.7 us, not
+    // 32.3, 2048 tokens 8.9 and 9.9, 1024 and 512 (5 MB) the same, 200 (2 MB) too.  What comes next then reads them from memory: with the
+    // write of the keys into a cache behind it 8192 tokens take 42.6 and 43.9, 2048 13.8 and 14.8, 1024 10.1 and 11.2; with that and
+    // attention, 2048 tokens 111.0 and 110.4.  A copy of all outputs loses more than was won: 8192 62.0 and 55.7, 2048 20.2 and 18.8.
+    // Loads that go past the caches, too, gain 2 % at the largest and lose a quarter at the others.
     const bool past = v * es == 16 && tokens * a.heads * static_cast<int64_t>(d) * es >= kPastBytes;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e;
