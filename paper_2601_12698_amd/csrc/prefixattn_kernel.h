@@ -110,27 +110,30 @@ __device__ __forceinline__ float other_row_sum(float x) { const pair p = with_ro
 // again with SAFE: the value becomes a zero in LDS, and `first` keeps, for each element, the first key at which it was NaN, +inf or
 // -inf.  Rows see the keys up to a last one: those from that first key on get the value added to their sum.  Looking at the sums costs
 // a meeting of the waves, where there are several queries a sequence: 2 x 64 queries of 32 heads over 1000 and 1000 keys 0.4 us of 17
-// (e4m3, heads of 64), 1 of 39 (bf16, 256).  Looking through every such tile as it is staged takes 2 of 17 and 3 of 39.
+// (e4m3, heads of 64), 0.6 of 39 (bf16, 256), 2 x 2 over 301 and 17 0.35 of 8.  Looking through every such tile as it is staged takes 2
+// of 17 and 3 of 39.
 template <int DT, int DP>
 struct Strays {
     static constexpr uint32_t EXPONENT = DT == DT_BF16 ? 0x7f80u : 0x7c00u;
     int32_t first[3][DP];
     int32_t odd[16];                                            // of each wave: a sum was not finite
 
-    // Whether the workgroup has to go over its keys again; if so, ready for that.
-    template <int WAVES, int N, typename V>
-    __device__ __forceinline__ bool found(const V (&o)[N], int wave, bool mine)
+    // Each wave says whether one of its sums is not finite (look); the waves meet; if one said so, all go over the keys again (found).
+    template <int N, typename V>
+    __device__ __forceinline__ void look(const V (&o)[N], int wave, bool mine)
     {
         constexpr int EACH = sizeof(V) / 4;
-        float none[4] = {0, 0, 0, 0};
+        float top[2] = {0, 0};                                  // NaN if one is
 #pragma unroll
         for (int t = 0; t < N; ++t)
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) none[i % 4] = __builtin_fmaf(o[t][i], 0.0f, none[i % 4]);
-        const float all = (none[0] + none[1]) + (none[2] + none[3]);
-        const bool some = __any(mine && all != all);
+            for (int i = 0; i < EACH; ++i) top[i / 2 % 2] = larger(top[i / 2 % 2], __builtin_fabsf(o[t][i]));
+        const bool some = __any(mine && !(larger(top[0], top[1]) < __builtin_huge_valf()));
         if (threadIdx.x % 64 == 0) odd[wave] = some;
-        __syncthreads();
+    }
+    template <int WAVES>
+    __device__ __forceinline__ bool found()
+    {
         int32_t any = 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) any |= odd[w];
@@ -176,13 +179,12 @@ __device__ __forceinline__ int thread()
 struct Share {
     addr_t table, table2;
     int32_t turn, head, token0, row0, rows, first, end, part, last0;
-    int32_t sure;                                               // all rows see the keys up to this one; kAll if those are all
 };
 constexpr int32_t kAll = 0x7fffffff;
-// A suffix's `sure`, once its other members are set: the last key of the tile's first row.
-__device__ __forceinline__ int32_t sure_of(const AttnArgs& a, const Share& s)
+// The last key that all queries of a suffix's sequence see; kAll if those are all of the share's.
+__device__ __forceinline__ int32_t sure_of(const Share& s)
 {
-    const int32_t last = max(s.last0 + s.row0 / a.group, s.turn < kAll ? s.turn - 1 : -1);
+    const int32_t last = max(s.last0, s.turn < kAll ? s.turn - 1 : -1);
     return last >= s.end - 1 ? kAll : last;
 }
 __device__ __forceinline__ int32_t page_at(const AttnArgs& a, const Share& s, int32_t key)
@@ -257,7 +259,7 @@ struct Few {
     static constexpr int JOIN_LDS = WAVES * (WAVE_LDS > ROWS * OROW * 4 ? WAVE_LDS : ROWS * OROW * 4);
     // Eight waves' 256 registers do not hold keys and values of 32 x 256 elements in 16 bits, sums and queries: the queries stay in LDS,
     // what follows from the lane is made anew in every turn and after the last, and the places of values are scalars until they are
-    // loaded from (32 x 8 heads over a page and 500 fp16 keys at most 19.1 us; with a place for each lane, and so scratch memory between
+    // loaded from (32 x 8 heads over a page and 500 fp16 keys at most 19.3 us; with a place for each lane, and so scratch memory between
     // the loads, 22.4; with the queries in registers, too, 32.4).
     static constexpr bool Q_LDS = !CODES && DP > 128 && WAVES == 8;
     static constexpr int QROW = DP * 2 + 32;
@@ -348,28 +350,24 @@ struct Few {
     template <bool SAFE>
     __device__ __forceinline__ void pass(const AttnArgs& a, const Share& s, int32_t page0, char* lds, f32x4 (&o)[DP / 16], float& m, float& l)
     {
-        const int tid = thread<SAFE>(), lane = tid & 63, wave = tid >> 6, g = lane >> 4;
+        const int first = thread<SAFE>(), lane = first & 63, wave = first >> 6;
         const Row row = row_of(a, s, lane & 15);
         if constexpr (SAFE) page0 = s.first + TILE * wave < s.end ? page_of(a, s, s.first + TILE * wave, lane) : 0;
         T8 q[NC];
-        const char* const at_q = lds + JOIN_LDS + (lane & 15) * QROW + 16 * g;
         if constexpr (Q_LDS) {
             static_assert(NC == WAVES, "a wave brings one piece of the queries");
-            *reinterpret_cast<T8*>(lds + JOIN_LDS + (lane & 15) * QROW + 64 * wave + 16 * g) = query_piece<DT>(a, row, 32 * wave + 8 * g);
+            *reinterpret_cast<T8*>(lds + JOIN_LDS + (lane & 15) * QROW + 64 * wave + 16 * (lane >> 4)) = query_piece<DT>(a, row, 32 * wave + 8 * (lane >> 4));
             __syncthreads();
         } else
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int32_t e = CODES ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
+            const int32_t e = CODES ? 64 * (c >> 1) + 16 * (lane >> 4) + 8 * (c & 1) : 32 * c + 8 * (lane >> 4);
             q[c] = query_piece<DT>(a, row, e);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = f32x4{0, 0, 0, 0};
         m = kNone, l = 0.0f;
         const float lag = fminf(kLazy / a.c, kMost);
-        char* mine = lds + wave * WAVE_LDS;
-        // where this lane's 8 bytes of a transposing read begin: key 4 g + (lane % 16) / 4 of 16, elements 4 (lane % 4) of 16
-        const char* from = mine + (4 * g + ((lane & 15) >> 2)) * VROW + 8 * (lane & 3);
 
         int32_t key0 = s.first + TILE * wave, page = 0;
         if (key0 < s.end) {
@@ -379,8 +377,11 @@ struct Few {
         while (key0 < s.end) {
             // made anew in every turn, so that what follows from it is not held in registers (from where it would go to scratch memory,
             // whose loads wait for those of keys and values)
-            int here = lane;
-            if constexpr (Q_LDS) asm volatile("" : "+v"(here));
+            const int tid = thread<Q_LDS>(), here = tid & 63, g = here >> 4;
+            char* const mine = lds + (tid >> 6) * WAVE_LDS;
+            const char* const at_q = lds + JOIN_LDS + (here & 15) * QROW + 16 * g;
+            // where this lane's 8 bytes of a transposing read begin: key 4 g + (lane % 16) / 4 of 16, elements 4 (lane % 4) of 16
+            const char* const from = mine + (4 * g + ((here & 15) >> 2)) * VROW + 8 * (here & 3);
             clear(a, here);
             // values to LDS, as elements
 #pragma unroll
@@ -427,12 +428,12 @@ struct Few {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (!((mine_there >> (16 * t + r)) & 1) || 16 * t + r > last) z[t][r] = kNone;
-                if (SAFE && now + TILE - 1 > s.sure) {
+                if (SAFE && now + TILE - 1 > sure_of(s)) {
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
                     for (int at = here / (DP / 8); at < TILE; at += 64 / (DP / 8))
-                        if (now + at > s.sure) reinterpret_cast<St*>(lds + LDS)->take_out(mine + at * VROW + 16 * (here % (DP / 8)), now + at, 8 * (here % (DP / 8)));
+                        if (now + at > sure_of(s)) reinterpret_cast<St*>(lds + LDS)->take_out(mine + at * VROW + 16 * (here % (DP / 8)), now + at, 8 * (here % (DP / 8)));
                 }
             }
             float top = z[0][0];
@@ -477,8 +478,10 @@ struct Few {
         const int tid = thread<true>(), lane = tid & 63, wave = tid >> 6, g = lane >> 4;
         St* const strays = reinterpret_cast<St*>(lds + LDS);
         bool strayed = false;
-        if (SUFFIX && __builtin_expect(s.sure < kAll, 0)) {     // said to be rare, or the pass above gets fewer registers
-            strayed = strays->template found<WAVES>(o, wave, true);
+        if (SUFFIX && __builtin_expect(sure_of(s) < kAll, !Q_LDS)) {     // where registers are few, said to be rare: the pass above gets them
+            strays->look(o, wave, true);
+            __syncthreads();
+            strayed = strays->template found<WAVES>();
             if (__builtin_expect(strayed, 0)) Few().template pass<true>(a, s, 0, lds, o, m, l);
         }
 
@@ -666,7 +669,7 @@ struct Many {
         const int b = piece() * (CODES ? 2 : 1);
 #pragma unroll 1
         for (int key = key_of(0); key < TILE; key += THREADS / PIECES)
-            if (key0 + key > s.sure)
+            if (key0 + key > sure_of(s))
 #pragma unroll 1
                 for (int h = 0; h < (CODES ? 2 : 1); ++h) reinterpret_cast<St*>(lds + LDS)->take_out(buf + TILE * KROW + key * VROW + 16 * (b + h), key0 + key, 8 * (b + h));
     }
@@ -782,7 +785,7 @@ struct Many {
             if constexpr (!ONE) ask(odd, s.first + TILE);
             even.clear(a);
             even.stage(lds);
-            if (SAFE && s.first + TILE - 1 > s.sure) look_through(s, s.first, lds, lds);
+            if (SAFE && s.first + TILE - 1 > sure_of(s)) look_through(s, s.first, lds, lds);
             if constexpr (ONE) ask(even, s.first + TILE);
             __syncthreads();
             // one turn: `key0`'s tile is in `buf`, the next one arrives in `next`, the one after is asked for into `after`
@@ -792,7 +795,7 @@ struct Many {
                 if (key0 + TILE < s.end) {
                     next.clear(a);
                     next.stage(other);
-                    if (SAFE && key0 + 2 * TILE - 1 > s.sure) look_through(s, key0 + TILE, other, lds);
+                    if (SAFE && key0 + 2 * TILE - 1 > sure_of(s)) look_through(s, key0 + TILE, other, lds);
                 }
                 if constexpr (ONE) ask(after, key0 + 2 * TILE);
                 __syncthreads();
@@ -820,8 +823,10 @@ struct Many {
         pass<false>(a, s, row, busy, lds, o, m, l);
         St* const strays = reinterpret_cast<St*>(lds + LDS);
         bool strayed = false;
-        if (SUFFIX && __builtin_expect(s.sure < kAll, 0)) {
-            strayed = strays->template found<WAVES>(o, wave, busy);
+        if (SUFFIX && sure_of(s) < kAll) {
+            strays->look(o, wave, busy);
+            __syncthreads();
+            strayed = strays->template found<WAVES>();
             if (__builtin_expect(strayed, 0)) pass<true>(a, s, row, busy, lds, o, m, l);
         }
         if constexpr (KS == 2) {
@@ -937,7 +942,7 @@ __global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW 
         s.first = split * a.prefix_chunk;
         s.end = min(s.first + a.prefix_chunk, a.prefix_len);
         s.part = split;
-        s.last0 = s.sure = kAll;
+        s.last0 = kAll;
         if constexpr (PREFIX == FEW || PREFIX == FEW_8) P().template run<false>(a, s, P::page_of(a, s, s.first + P::TILE * (threadIdx.x >> 6), threadIdx.x & 63), lds);
         else P().template run<false>(a, s, lds);
         return;
@@ -970,14 +975,12 @@ __global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW 
         s.end = a.inline_len ? a.inline_len + keys : min(s.first + a.suffix_chunk, keys);
         s.last0 = a.inline_len + keys - a.q_len;
         if (s.first >= s.end && !a.finish) return;              // the joining kernel knows the length, too
-        s.sure = sure_of(a, s);
         S().template run<true>(a, s, page0, lds);
     } else {
         const int32_t keys = min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), room);
         s.end = min(s.first + a.suffix_chunk, keys);
         s.last0 = keys - a.q_len;
         if (s.first >= s.end && !a.finish) return;
-        s.sure = sure_of(a, s);
         S().template run<true>(a, s, lds);
     }
 }
