@@ -39,6 +39,7 @@ DEVICE_FLAGS = [f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-ffp-co
 # costs a tiny one.  Not for the merges' grid instances, whose launches are small (328 x 96 fp16 1.78 us without, 1.94 with).
 PRELOAD_FLAGS = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra"]
+SERVING_HEADERS = ("rotary.h", "kvcache.h", "prefixattn.h", "kvmove.h", "treeaccept.h", "treeattn.h", "logits.h")
 INCLUDES = ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", BUILD]
 
 
@@ -100,7 +101,7 @@ def _compile_native(force: bool) -> None:
     from .binding import torch_identity
     tdir, identity = os.path.dirname(torch.__file__), torch_identity()
     src, obj = os.path.join(CSRC, "native_calls.cpp"), os.path.join(BUILD, "native_calls.cpp.o")
-    if not force and _newer(NATIVE, src, *(os.path.join(ROOT, "include", h) for h in ("addrms.h", "rotary.h", "kvcache.h", "prefixattn.h"))):
+    if not force and _newer(NATIVE, src, *(os.path.join(ROOT, "include", h) for h in ("addrms.h", *SERVING_HEADERS))):
         with open(NATIVE, "rb") as f:
             if identity.encode() in f.read():
                 return
@@ -123,15 +124,17 @@ def build_native(force: bool) -> None:
 
 
 def _compile_serving(force: bool, jobs: int, hdrs) -> list:
-    """Objects of the operators around a decode step's attention.  The attention kernels are one unit for each element type,
-    cache format and padded head size, so that they compile side by side."""
-    deps = [*hdrs, os.path.join(CSRC, "serving_internal.h"), *(os.path.join(ROOT, "include", h) for h in ("rotary.h", "kvcache.h", "prefixattn.h"))]
-    attn = [os.path.join(CSRC, "prefixattn_kernel.h"), os.path.join(CSRC, "prefixattn_args.h")]
-    units = [(n, n[:-4], [], []) for n in ("rotary.hip", "kvcache.hip")] + [("prefixattn.hip", "prefixattn", [], attn)]
-    for dt in (0, 1):
-        for fmt in (0, 1):
-            for dp in (64, 128, 256):
-                units.append(("prefixattn_unit.hip", f"prefixattn_d{dt}_f{fmt}_h{dp}", [f"-DUNIT_DT={dt}", f"-DUNIT_FORMAT={fmt}", f"-DUNIT_DP={dp}"], attn))
+    """Objects of the operators around a decode step's attention, and of those that check drafted tokens.  The attention kernels are
+    one unit for each element type, cache format and padded head size, so that they compile side by side."""
+    deps = [*hdrs, os.path.join(CSRC, "serving_internal.h"), *(os.path.join(ROOT, "include", h) for h in SERVING_HEADERS)]
+    attn = [os.path.join(CSRC, f) for f in ("prefixattn_kernel.h", "prefixattn_args.h", "prefixattn_plan.h", "prefixattn_join.h", "treeattn_kernel.h")]
+    units = [(n, n[:-4], [], []) for n in ("rotary.hip", "kvcache.hip", "kvmove.hip", "treeaccept.hip", "logits.hip")]
+    units += [("prefixattn.hip", "prefixattn", [], attn), ("treeattn.hip", "treeattn", [], attn)]
+    for op in ("prefixattn", "treeattn"):
+        for dt in (0, 1):
+            for fmt in (0, 1):
+                for dp in (64, 128, 256):
+                    units.append((f"{op}_unit.hip", f"{op}_d{dt}_f{fmt}_h{dp}", [f"-DUNIT_DT={dt}", f"-DUNIT_FORMAT={fmt}", f"-DUNIT_DP={dp}"], attn))
 
     def one(unit):
         src, name, defs, more = os.path.join(CSRC, unit[0]), unit[1], unit[2], unit[3]

@@ -18,8 +18,12 @@
 
 #include <cstdint>
 
+#include "kvmove.h"
+#include "logits.h"
 #include "prefixattn.h"
 #include "rotary.h"
+#include "treeaccept.h"
+#include "treeattn.h"
 
 namespace {
 
@@ -329,51 +333,66 @@ PyObject* kvcache_read(PyObject*, PyObject* const* a, Py_ssize_t n)
         });
     });
 }
+// What the calls of attention over a cache have in common: (q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_len,
+// suffix_pages, suffix_lens), then (out, lse, scale, dtype), and the workspace.
+struct Attention {
+    Heads q;
+    Cache c;
+    void *first = nullptr, *own = nullptr, *lens = nullptr, *out = nullptr, *lse = nullptr, *work = nullptr, *stream = nullptr;
+    int64_t bytes = 0;
+    float scale = 0.0f;
+    prefixattn_shape shape;
+};
+// `q_len` queries a sequence.
+bool attention_of(PyObject* const* a, PyObject* const* after, PyObject* workspace, int64_t q_len, Attention* x)
+{
+    int dt;
+    int64_t prefix;
+    if (!format(after[3], &dt) || dt > 1 || !whole(a[6], &prefix) || !PyFloat_CheckExact(after[2])) return false;
+    const at::Tensor* q = device_tensor(a[0], kX[dt], 3);
+    Cache& c = x->c;
+    if (!q || !cache_of(a + 1, dt, *q, &c)) return false;
+    const int64_t rows = q->size(0), hq = q->size(1);
+    if (q_len < 1 || !small(q_len) || rows % q_len || !small(rows) || !small(hq) || prefix < 0 || !small(prefix) || !heads_of(a[0], kX[dt], nullptr, rows, hq, c.d, &x->q))
+        return false;
+    if (prefix) {
+        const at::Tensor* t = device_tensor(a[5], at::kInt, 1, q);
+        if (!t || !t->is_contiguous() || t->size(0) < (prefix + c.page - 1) / c.page) return false;
+        x->first = t->data_ptr();
+    }
+    int64_t width = 0;
+    if (a[7] != Py_None) {
+        const at::Tensor* t = device_tensor(a[7], at::kInt, 2, q);
+        if (!t || t->size(1) == 0) return false;
+        width = t->size(1);
+        if (!whole_data(a[7], at::kInt, *q, &x->own, rows / q_len, width) || !whole_data(a[8], at::kInt, *q, &x->lens, rows / q_len)) return false;
+    }
+    if (!whole_data(after[0], kX[dt], *q, &x->out, rows, hq, c.d) || (after[1] != Py_None && !whole_data(after[1], at::kFloat, *q, &x->lse, rows, hq)) ||
+        !THPVariable_CheckExact(workspace))
+        return false;
+    const at::Tensor& room = THPVariable_Unpack(workspace);
+    if (!room.is_cuda() || room.get_device() != q->get_device() || !room.is_contiguous()) return false;
+    x->work = room.data_ptr();
+    x->bytes = room.numel() * static_cast<int64_t>(room.element_size());
+    prefixattn_shape& shape = x->shape;
+    shape.batch = static_cast<int32_t>(rows / q_len), shape.q_len = static_cast<int32_t>(q_len), shape.q_heads = static_cast<int32_t>(hq);
+    shape.kv_heads = static_cast<int32_t>(c.heads), shape.d = static_cast<int32_t>(c.d), shape.page_size = static_cast<int32_t>(c.page);
+    shape.pages = c.pages, shape.prefix_len = prefix, shape.suffix_width = width, shape.dtype = dt, shape.format = c.format;
+    x->scale = static_cast<float>(PyFloat_AS_DOUBLE(after[2]));
+    x->stream = stream_of(a[0]);
+    return true;
+}
 // (q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_len, suffix_pages, suffix_lens, out, lse, scale, dtype, q_len, workspace)
 PyObject* prefixattn_run(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject* {
-        int dt;
-        int64_t prefix, q_len;
-        if (n != 15 || !g_attend || !format(a[12], &dt) || dt > 1 || !whole(a[6], &prefix) || !whole(a[13], &q_len) || !PyFloat_CheckExact(a[11]))
-            return general();
-        const at::Tensor* q = device_tensor(a[0], kX[dt], 3);
-        Cache c;
-        Heads qh;
-        if (!q || !cache_of(a + 1, dt, *q, &c)) return general();
-        const int64_t rows = q->size(0), hq = q->size(1);
-        if (q_len < 1 || !small(q_len) || rows % q_len || !small(rows) || !small(hq) || prefix < 0 || !small(prefix) || !heads_of(a[0], kX[dt], nullptr, rows, hq, c.d, &qh))
-            return general();
-        void *first = nullptr, *own = nullptr, *lens = nullptr, *out, *lse = nullptr;
-        if (prefix) {
-            const at::Tensor* t = device_tensor(a[5], at::kInt, 1, q);
-            if (!t || !t->is_contiguous() || t->size(0) < (prefix + c.page - 1) / c.page) return general();
-            first = t->data_ptr();
-        }
-        int64_t width = 0;
-        if (a[7] != Py_None) {
-            const at::Tensor* t = device_tensor(a[7], at::kInt, 2, q);
-            if (!t || t->size(1) == 0) return general();
-            width = t->size(1);
-            if (!whole_data(a[7], at::kInt, *q, &own, rows / q_len, width) || !whole_data(a[8], at::kInt, *q, &lens, rows / q_len)) return general();
-        }
-        if (!whole_data(a[9], kX[dt], *q, &out, rows, hq, c.d) || (a[10] != Py_None && !whole_data(a[10], at::kFloat, *q, &lse, rows, hq)) ||
-            !THPVariable_CheckExact(a[14]))
-            return general();
-        const at::Tensor& room = THPVariable_Unpack(a[14]);
-        if (!room.is_cuda() || room.get_device() != q->get_device() || !room.is_contiguous()) return general();
-        void* work = room.data_ptr();
-        const int64_t bytes = room.numel() * static_cast<int64_t>(room.element_size());
-        prefixattn_shape shape;
-        shape.batch = static_cast<int32_t>(rows / q_len), shape.q_len = static_cast<int32_t>(q_len), shape.q_heads = static_cast<int32_t>(hq);
-        shape.kv_heads = static_cast<int32_t>(c.heads), shape.d = static_cast<int32_t>(c.d), shape.page_size = static_cast<int32_t>(c.page);
-        shape.pages = c.pages, shape.prefix_len = prefix, shape.suffix_width = width, shape.dtype = dt, shape.format = c.format;
-        const float scale = static_cast<float>(PyFloat_AS_DOUBLE(a[11]));
-        void* s = stream_of(a[0]);
-        return status([=, &qh, &shape] {
-            return g_attend(qh.data, qh.strides, c.k, c.v, static_cast<const uint8_t*>(c.ks), static_cast<const uint8_t*>(c.vs),
-                            static_cast<const int32_t*>(first), static_cast<const int32_t*>(own), static_cast<const int32_t*>(lens), out,
-                            static_cast<float*>(lse), scale, &shape, work, bytes, s);
+        int64_t q_len;
+        Attention x;
+        if (n != 15 || !g_attend || !whole(a[13], &q_len) || !attention_of(a, a + 9, a[14], q_len, &x)) return general();
+        return status([&x] {
+            return g_attend(x.q.data, x.q.strides, x.c.k, x.c.v, static_cast<const uint8_t*>(x.c.ks), static_cast<const uint8_t*>(x.c.vs),
+                            static_cast<const int32_t*>(x.first), static_cast<const int32_t*>(x.own), static_cast<const int32_t*>(x.lens), x.out,
+                            static_cast<float*>(x.lse), x.scale, &x.shape, x.work, x.bytes, x.stream);
         });
     });
 }
@@ -389,6 +408,174 @@ PyObject* bind_serving(PyObject*, PyObject* args)
     g_write = reinterpret_cast<decltype(g_write)>(static_cast<uintptr_t>(write));
     g_read = reinterpret_cast<decltype(g_read)>(static_cast<uintptr_t>(read));
     g_attend = reinterpret_cast<decltype(g_attend)>(static_cast<uintptr_t>(attend));
+    Py_RETURN_NONE;
+}
+
+// ---- the operators of a step that checks drafted tokens (drafting.py) ----------------------------------------------------------
+
+decltype(&::treeattn_run) g_tree;
+decltype(&::logits_run) g_logits;
+decltype(&::treeaccept_run) g_accept;
+decltype(&::kvmove_run) g_move;
+
+// (q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_len, suffix_pages, suffix_lens, masks, out, lse, scale, dtype, workspace)
+PyObject* treeattn_run(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        Attention x;
+        void* masks;
+        if (n != 15 || !g_tree || !THPVariable_CheckExact(a[0]) || !THPVariable_CheckExact(a[9])) return general();
+        const at::Tensor &q = THPVariable_Unpack(a[0]), &m = THPVariable_Unpack(a[9]);
+        if (m.dim() != 2 || m.size(0) < 1 || m.size(1) < 1 || !whole_data(a[9], at::kLong, q, &masks, m.size(0), m.size(1)) || q.dim() != 3 ||
+            q.size(0) != m.size(0) * m.size(1) || !attention_of(a, a + 10, a[14], m.size(1), &x))
+            return general();
+        return status([&x, masks] {
+            return g_tree(x.q.data, x.q.strides, x.c.k, x.c.v, static_cast<const uint8_t*>(x.c.ks), static_cast<const uint8_t*>(x.c.vs),
+                          static_cast<const int32_t*>(x.first), static_cast<const int32_t*>(x.own), static_cast<const int32_t*>(x.lens),
+                          static_cast<const int64_t*>(masks), x.out, static_cast<float*>(x.lse), x.scale, &x.shape, x.work, x.bytes, x.stream);
+        });
+    });
+}
+// A [rows, width] tensor whose rows may be any distance apart (width below 0: any).
+bool rows_of(PyObject* o, at::ScalarType type, const at::Tensor* as, int64_t rows, int64_t width, void** out, int64_t* stride, int64_t* has = nullptr)
+{
+    const at::Tensor* t = device_tensor(o, type, 2, as);
+    if (!t || t->size(0) != rows || (width >= 0 && t->size(1) != width) || (t->stride(1) != 1 && t->size(1) > 1)) return false;
+    *out = t->data_ptr();
+    *stride = t->stride(0);
+    if (has) *has = t->size(1);
+    return true;
+}
+// (logits, out, best, dtype, nodes, history, history_lens, prompt_lens, penalties, bias_tokens, bias_values, allowed, tree_tokens,
+//  tree_masks, workspace)
+PyObject* logits_run(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        int dt;
+        int64_t nodes, stride, out_stride = 0, words, width = 0;
+        void *x, *out = nullptr, *best = nullptr, *work = nullptr, *p;
+        if (n != 15 || !g_logits || !format(a[3], &dt) || dt == 2 || !whole(a[4], &nodes) || nodes < 1) return general();
+        const at::Tensor* t = device_tensor(a[0], kX[dt], 2);
+        if (!t || t->size(0) % nodes || !small(t->size(0))) return general();
+        const int64_t rows = t->size(0), vocab = t->size(1), batch = rows / nodes;
+        const auto none = [&](int i) { return a[i] == Py_None; };
+        if (!rows_of(a[0], kX[dt], nullptr, rows, vocab, &x, &stride) || (!none(1) && !rows_of(a[1], kX[dt], t, rows, vocab, &out, &out_stride)) ||
+            (!none(2) && !whole_data(a[2], at::kInt, *t, &best, rows)))
+            return general();
+        logits_lists l = {};
+        if (!none(5)) {
+            if (!rows_of(a[5], at::kInt, t, batch, -1, &p, &l.history_stride, &width) || !small(width)) return general();
+            l.history = static_cast<const int32_t*>(p), l.history_width = static_cast<int32_t>(width);
+            if (!whole_data(a[6], at::kInt, *t, &p, batch)) return general();
+            l.history_lens = static_cast<const int32_t*>(p);
+            if (!none(7)) {
+                if (!whole_data(a[7], at::kInt, *t, &p, batch)) return general();
+                l.prompt_lens = static_cast<const int32_t*>(p);
+            }
+        }
+        if (!none(8)) {
+            if (!whole_data(a[8], at::kFloat, *t, &p, batch, 3)) return general();
+            l.penalties = static_cast<const float*>(p);
+        }
+        if (!none(9)) {
+            if (!THPVariable_CheckExact(a[9]) || THPVariable_Unpack(a[9]).dim() != 2) return general();
+            const int64_t biases = THPVariable_Unpack(a[9]).size(1);
+            if (!small(biases) || !whole_data(a[9], at::kInt, *t, &p, batch, biases)) return general();
+            l.bias_tokens = static_cast<const int32_t*>(p), l.biases = static_cast<int32_t>(biases);
+            if (!whole_data(a[10], at::kFloat, *t, &p, batch, biases)) return general();
+            l.bias_values = static_cast<const float*>(p);
+        } else if (!none(10)) {
+            return general();
+        }
+        if (!none(11)) {
+            if (!rows_of(a[11], at::kInt, t, rows, -1, &p, &l.allowed_stride, &words) || words < (vocab + 31) / 32) return general();
+            l.allowed = static_cast<const uint32_t*>(p);
+        }
+        if (none(12) != none(13)) return general();
+        if (!none(12)) {
+            if (!whole_data(a[12], at::kInt, *t, &p, batch, nodes)) return general();
+            l.tree_tokens = static_cast<const int32_t*>(p);
+            if (!whole_data(a[13], at::kLong, *t, &p, batch, nodes)) return general();
+            l.tree_masks = static_cast<const int64_t*>(p);
+        }
+        int64_t bytes = 0;
+        if (best) {
+            if (!THPVariable_CheckExact(a[14])) return general();
+            const at::Tensor& room = THPVariable_Unpack(a[14]);
+            if (!room.is_cuda() || room.get_device() != t->get_device() || !room.is_contiguous()) return general();
+            work = room.data_ptr();
+            bytes = room.numel() * static_cast<int64_t>(room.element_size());
+        }
+        void* s = stream_of(a[0]);
+        return status([=, &l] {
+            return g_logits(x, stride, out, out_stride, static_cast<int32_t*>(best), batch, static_cast<int32_t>(nodes), vocab, dt, &l, work, bytes, s);
+        });
+    });
+}
+// (chosen, tokens, masks, suffix_pages, suffix_lens, page_size, pages, path, count, next_token, from_slots, to_slots)
+PyObject* treeaccept_run(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        int64_t page, pages, width = 0;
+        if (n != 12 || !g_accept || !whole(a[5], &page) || !whole(a[6], &pages) || !small(page) || page < 1) return general();
+        const at::Tensor *m = device_tensor(a[2], at::kLong, 2), *way = m ? device_tensor(a[7], at::kInt, 2, m) : nullptr;
+        if (!way) return general();
+        const int64_t batch = m->size(0), nodes = m->size(1), depth = way->size(1);
+        void *chosen, *tokens, *masks, *table = nullptr, *lens = nullptr, *path, *count, *next, *from = nullptr, *to = nullptr;
+        if (!small(nodes) || !small(depth) || !whole_data(a[0], at::kInt, *m, &chosen, batch, nodes) || !whole_data(a[1], at::kInt, *m, &tokens, batch, nodes) ||
+            !whole_data(a[2], at::kLong, *m, &masks, batch, nodes) || !whole_data(a[7], at::kInt, *m, &path, batch, depth) ||
+            !whole_data(a[8], at::kInt, *m, &count, batch) || !whole_data(a[9], at::kInt, *m, &next, batch) || (a[10] == Py_None) != (a[11] == Py_None))
+            return general();
+        if (a[10] != Py_None) {
+            if (!THPVariable_CheckExact(a[3]) || THPVariable_Unpack(a[3]).dim() != 2) return general();
+            width = THPVariable_Unpack(a[3]).size(1);
+            if (!whole_data(a[3], at::kInt, *m, &table, batch, width) || !whole_data(a[4], at::kInt, *m, &lens, batch) ||
+                !whole_data(a[10], at::kLong, *m, &from, batch, depth) || !whole_data(a[11], at::kLong, *m, &to, batch, depth))
+                return general();
+        }
+        void* s = stream_of(a[2]);
+        return status([=] {
+            return g_accept(static_cast<const int32_t*>(chosen), static_cast<const int32_t*>(tokens), static_cast<const int64_t*>(masks),
+                            static_cast<const int32_t*>(table), static_cast<const int32_t*>(lens), static_cast<int32_t*>(path), static_cast<int32_t*>(count),
+                            static_cast<int32_t*>(next), static_cast<int64_t*>(from), static_cast<int64_t*>(to), batch, static_cast<int32_t>(nodes),
+                            static_cast<int32_t>(depth), width, pages, static_cast<int32_t>(page), s);
+        });
+    });
+}
+// (k_pages, v_pages, k_scale, v_scale, from_slots, to_slots, dtype)
+PyObject* kvmove_run(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        int dt;
+        Cache c;
+        void *from, *to;
+        if (n != 7 || !g_move || !format(a[6], &dt) || dt > 1 || !THPVariable_CheckExact(a[0])) return general();
+        const at::Tensor& k = THPVariable_Unpack(a[0]);
+        if (!cache_of(a, dt, k, &c)) return general();
+        const at::Tensor* f = device_tensor(a[4], at::kLong, 2, &k);
+        if (!f) return general();
+        const int64_t groups = f->size(0), tokens = f->size(1);
+        if (!small(tokens) || !whole_data(a[4], at::kLong, k, &from, groups, tokens) || !whole_data(a[5], at::kLong, k, &to, groups, tokens)) return general();
+        void* s = stream_of(a[0]);
+        return status([=] {
+            return g_move(c.k, c.v, static_cast<uint8_t*>(c.ks), static_cast<uint8_t*>(c.vs), static_cast<const int64_t*>(from), static_cast<const int64_t*>(to),
+                          groups, static_cast<int32_t>(tokens), static_cast<int32_t>(c.heads), static_cast<int32_t>(c.d), c.pages, static_cast<int32_t>(c.page),
+                          dt, c.format, s);
+        });
+    });
+}
+// (formats, addresses of treeattn_run, logits_run, treeaccept_run and kvmove_run)
+PyObject* bind_drafting(PyObject*, PyObject* args)
+{
+    PyObject* formats;
+    unsigned long long tree, logits, accept, move;
+    if (!PyArg_ParseTuple(args, "O!KKKK", &PyDict_Type, &formats, &tree, &logits, &accept, &move)) return nullptr;
+    Py_INCREF(formats);
+    Py_XSETREF(g_formats, formats);
+    g_tree = reinterpret_cast<decltype(g_tree)>(static_cast<uintptr_t>(tree));
+    g_logits = reinterpret_cast<decltype(g_logits)>(static_cast<uintptr_t>(logits));
+    g_accept = reinterpret_cast<decltype(g_accept)>(static_cast<uintptr_t>(accept));
+    g_move = reinterpret_cast<decltype(g_move)>(static_cast<uintptr_t>(move));
     Py_RETURN_NONE;
 }
 
@@ -422,6 +609,11 @@ PyMethodDef g_methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                            {"kvcache_write", FAST(kvcache_write), nullptr},
                            {"kvcache_read", FAST(kvcache_read), nullptr},
                            {"prefixattn_run", FAST(prefixattn_run), nullptr},
+                           {"bind_drafting", bind_drafting, METH_VARARGS, nullptr},
+                           {"treeattn_run", FAST(treeattn_run), nullptr},
+                           {"logits_run", FAST(logits_run), nullptr},
+                           {"treeaccept_run", FAST(treeaccept_run), nullptr},
+                           {"kvmove_run", FAST(kvmove_run), nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -18,6 +18,7 @@ struct AttnArgs {
     int32_t finish;                                   // the suffixes' workgroups join the prefix's parts to their own, and write the output
     int32_t q_wide;                                   // queries can be read 16 bytes at a time
     float c;                                          // scale * log2(e): weights are powers of 2
+    uint64_t masks;                                   // of a tree's nodes (include/treeattn.h), whose keys follow suffix_lens
 };
 
 // Forms of a workgroup: 16 rows whose four (FEW_8: eight) waves take keys in turn; 64, 128 or 256 rows that share their keys (64:
@@ -31,7 +32,7 @@ constexpr int kChunkStep = 128;                       // splits begin at multipl
 constexpr int kFinishSplits = 64;                     // of a prefix that is joined by the suffixes' workgroups: a part a lane
 constexpr int kMaxSplits = 256;                       // of a prefix, and of a suffix
 
-// One for each element type, format and padded head size (prefixattn_unit.hip).
+// One for each element type, format and padded head size (prefixattn_unit.hip; for trees treeattn_unit.hip).
 typedef hipError_t (*AttnLaunch)(const AttnArgs&, int prefix_form, int suffix_form, unsigned blocks, hipStream_t);
 #define ATTN_UNIT_NAME(dt, fmt, dp) attn_launch_d##dt##_f##fmt##_h##dp
 #define ATTN_UNIT(dt, fmt, dp) ATTN_UNIT_NAME(dt, fmt, dp)
@@ -41,5 +42,13 @@ typedef hipError_t (*AttnLaunch)(const AttnArgs&, int prefix_form, int suffix_fo
     hipError_t ATTN_UNIT(dt, fmt, 256)(const AttnArgs&, int, int, unsigned, hipStream_t);
 ATTN_DECLARE(0, 0) ATTN_DECLARE(0, 1) ATTN_DECLARE(1, 0) ATTN_DECLARE(1, 1)
 #undef ATTN_DECLARE
+#define TREE_UNIT_NAME(dt, fmt, dp) tree_launch_d##dt##_f##fmt##_h##dp
+#define TREE_UNIT(dt, fmt, dp) TREE_UNIT_NAME(dt, fmt, dp)
+#define TREE_DECLARE(dt, fmt) \
+    hipError_t TREE_UNIT(dt, fmt, 64)(const AttnArgs&, int, int, unsigned, hipStream_t);  \
+    hipError_t TREE_UNIT(dt, fmt, 128)(const AttnArgs&, int, int, unsigned, hipStream_t); \
+    hipError_t TREE_UNIT(dt, fmt, 256)(const AttnArgs&, int, int, unsigned, hipStream_t);
+TREE_DECLARE(0, 0) TREE_DECLARE(0, 1) TREE_DECLARE(1, 0) TREE_DECLARE(1, 1)
+#undef TREE_DECLARE
 
 }  // namespace serving

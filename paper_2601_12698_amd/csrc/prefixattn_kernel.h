@@ -111,11 +111,13 @@ __device__ __forceinline__ float other_row_sum(float x) { const pair p = with_ro
 // -inf.  Rows see the keys up to a last one: those from that first key on get the value added to their sum.  Looking at the sums costs
 // a meeting of the waves, where there are several queries a sequence: 2 x 64 queries of 32 heads over 1000 and 1000 keys 0.4 us of 17
 // (e4m3, heads of 64), 0.6 of 39 (bf16, 256), 2 x 2 over 301 and 17 0.35 of 8.  Looking through every such tile as it is staged takes 2
-// of 17 and 3 of 39.
-template <int DT, int DP>
-struct Strays {
+// of 17 and 3 of 39.  TREE: such keys are nodes of a tree (include/treeattn.h), and `nodes` keeps for each
+// element those at which it was +inf or NaN, and those at which it was -inf or NaN.
+template <int DP, bool TREE> struct StrayKeys { int32_t first[3][DP]; };
+template <int DP> struct StrayKeys<DP, true> { uint64_t nodes[2][DP]; };
+template <int DT, int DP, bool TREE = false>
+struct Strays : StrayKeys<DP, TREE> {
     static constexpr uint32_t EXPONENT = DT == DT_BF16 ? 0x7f80u : 0x7c00u;
-    int32_t first[3][DP];
     int32_t odd[16];                                            // of each wave: a sum was not finite
 
     // Each wave says whether one of its sums is not finite (look); the waves meet; if one said so, all go over the keys again (found).
@@ -138,11 +140,14 @@ struct Strays {
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) any |= odd[w];
         if (__builtin_expect(any == 0, 1)) return false;
-        for (int i = threadIdx.x; i < 3 * DP; i += 64 * WAVES) first[0][i] = 0x7fffffff;
+        for (int i = threadIdx.x; i < (TREE ? 2 : 3) * DP; i += 64 * WAVES) {
+            if constexpr (TREE) this->nodes[0][i] = 0;
+            else this->first[0][i] = 0x7fffffff;
+        }
         __syncthreads();
         return true;
     }
-    // Eight elements in LDS, those of `key` from e on.
+    // Eight elements in LDS, those of `key` (TREE: of the node of this number) from e on.
     __device__ __forceinline__ void take_out(char* at, int32_t key, int32_t e)
     {
 #pragma unroll 1
@@ -151,16 +156,24 @@ struct Strays {
             const uint32_t w = *p;
             if ((w & EXPONENT) != EXPONENT) continue;
             const int kind = (w & (EXPONENT ^ 0x7fffu)) ? 0 : w >> 15 ? 2 : 1;
-            atomicMin(&first[kind][e + i], key);
+            if constexpr (TREE) {
+                if (kind != 2) atomicOr(reinterpret_cast<unsigned long long*>(&this->nodes[0][e + i]), 1ull << key);
+                if (kind != 1) atomicOr(reinterpret_cast<unsigned long long*>(&this->nodes[1][e + i]), 1ull << key);
+            } else atomicMin(&this->first[kind][e + i], key);
             *p = 0;
         }
     }
-    // What element e of a row's sum gets.
-    __device__ __forceinline__ float of(int32_t e, int32_t last) const
+    // What element e of a row's sum gets; the row sees keys up to `last` (TREE: and the nodes `seen`).
+    __device__ __forceinline__ float of(int32_t e, int32_t last, uint64_t seen) const
     {
-        float x = first[1][e] <= last ? __builtin_huge_valf() : 0.0f;
-        x = first[2][e] <= last ? x - __builtin_huge_valf() : x;
-        return first[0][e] <= last ? __builtin_nanf("") : x;
+        if constexpr (TREE) {
+            const float x = this->nodes[0][e] & seen ? __builtin_huge_valf() : 0.0f;
+            return this->nodes[1][e] & seen ? x - __builtin_huge_valf() : x;         // both: NaN
+        } else {
+            float x = this->first[1][e] <= last ? __builtin_huge_valf() : 0.0f;
+            x = this->first[2][e] <= last ? x - __builtin_huge_valf() : x;
+            return this->first[0][e] <= last ? __builtin_nanf("") : x;
+        }
     }
 };
 
@@ -210,6 +223,17 @@ __device__ __forceinline__ Row row_of(const AttnArgs& a, const Share& s, int32_t
     row.q = token * a.q_token + head * a.q_head;
     return row;
 }
+// Of a tree: the nodes that row r of a share sees, whose keys follow last0, and which of the 64 keys from key0 on it sees with that.
+__device__ __forceinline__ uint64_t nodes_of(const AttnArgs& a, const Share& s, int32_t r)
+{
+    return at_global<const uint64_t>(a.masks)[s.token0 + (s.row0 + (r < s.rows ? r : 0)) / a.group] & full_of(a.q_len);
+}
+__device__ __forceinline__ uint64_t seen_from(const Share& s, uint64_t nodes, int32_t key0)
+{
+    const int32_t node = key0 - 1 - s.last0;                    // that key's number among the nodes; below 0 it is before them
+    if (node >= 0) return node < 64 ? nodes >> node : 0;
+    return node > -64 ? nodes << -node | full_of(-node) : ~0ull;
+}
 
 // Where a key's elements and its scale lie.  Where its page is not in the cache, or the key is beyond the share's end, callers
 // take page 0 and set the piece to zeros afterwards: loads stand in no branch, so that all of a tile's are under way together.
@@ -239,7 +263,7 @@ __device__ __forceinline__ typename mat<DT>::T8 query_piece(const AttnArgs& a, c
     return row.in && e < a.d ? x : T8{};
 }
 
-template <int DT, int FORMAT, int DP, int WAVES>
+template <int DT, int FORMAT, int DP, int WAVES, bool TREE = false>
 struct Few {
     typedef mat<DT> M;
     typedef typename M::T T;
@@ -263,8 +287,10 @@ struct Few {
     // the loads, 22.4; with the queries in registers, too, 32.4).
     static constexpr bool Q_LDS = !CODES && DP > 128 && WAVES == 8;
     static constexpr int QROW = DP * 2 + 32;
-    static constexpr int LDS = JOIN_LDS + (Q_LDS ? ROWS * QROW : 0);
-    typedef Strays<DT, DP> St;
+    static constexpr int MASKS_LDS = JOIN_LDS + ROWS * QROW;    // and so do a tree's masks
+    static constexpr int LDS = JOIN_LDS + (Q_LDS ? ROWS * (QROW + (TREE ? 8 : 0)) : 0);
+    typedef Strays<DT, DP, TREE> St;
+    static __device__ __forceinline__ int32_t nodes_at(const Share& s) { return TREE ? s.last0 + 1 : 0; }
     static constexpr int SUFFIX_LDS = LDS + static_cast<int>(sizeof(St));
     // What the waves tell each other at the end, once for both kinds of shares.
     struct Ends {
@@ -352,11 +378,13 @@ struct Few {
     {
         const int first = thread<SAFE>(), lane = first & 63, wave = first >> 6;
         const Row row = row_of(a, s, lane & 15);
+        const uint64_t nodes = TREE ? nodes_of(a, s, lane & 15) : 0;
         if constexpr (SAFE) page0 = s.first + TILE * wave < s.end ? page_of(a, s, s.first + TILE * wave, lane) : 0;
         T8 q[NC];
         if constexpr (Q_LDS) {
             static_assert(NC == WAVES, "a wave brings one piece of the queries");
             *reinterpret_cast<T8*>(lds + JOIN_LDS + (lane & 15) * QROW + 64 * wave + 16 * (lane >> 4)) = query_piece<DT>(a, row, 32 * wave + 8 * (lane >> 4));
+            if constexpr (TREE) *reinterpret_cast<uint64_t*>(lds + MASKS_LDS + 8 * (lane & 15)) = nodes;
             __syncthreads();
         } else
 #pragma unroll
@@ -421,8 +449,9 @@ struct Few {
                 page = page_of(a, s, key0 + WAVES * TILE, here);
             }
             if (there != 0xffffffffu || now + TILE - 1 > s.last0) {
-                const uint32_t mine_there = there >> (4 * g);   // this lane's keys, shifted so that each is a fixed bit
-                const int32_t last = row.last - now - 4 * g;
+                // this lane's keys, shifted so that each is a fixed bit
+                const uint32_t mine_there = (TREE ? there & static_cast<uint32_t>(seen_from(s, Q_LDS ? *reinterpret_cast<const uint64_t*>(lds + MASKS_LDS + 8 * (here & 15)) : nodes, now)) : there) >> (4 * g);
+                const int32_t last = TREE ? TILE : row.last - now - 4 * g;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -433,7 +462,7 @@ struct Few {
                     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
                     for (int at = here / (DP / 8); at < TILE; at += 64 / (DP / 8))
-                        if (now + at > sure_of(s)) reinterpret_cast<St*>(lds + LDS)->take_out(mine + at * VROW + 16 * (here % (DP / 8)), now + at, 8 * (here % (DP / 8)));
+                        if (now + at > sure_of(s)) reinterpret_cast<St*>(lds + LDS)->take_out(mine + at * VROW + 16 * (here % (DP / 8)), now + at - nodes_at(s), 8 * (here % (DP / 8)));
                 }
             }
             float top = z[0][0];
@@ -547,7 +576,7 @@ struct Few {
             for (int w = 1; w < WAVES; ++w) x += *reinterpret_cast<const f32x4*>(join + (w * ROWS + r) * OROW + e);
             if (SUFFIX && strayed)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] += strays->of(e + j, row.last);
+                for (int j = 0; j < 4; ++j) x[j] += strays->of(e + j, row.last, TREE ? nodes_of(a, s, r) : 0);
             if (!finish) {
                 *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + (s.part * rows + global) * a.d + e) = x;
                 continue;
@@ -571,7 +600,7 @@ struct Few {
     }
 };
 
-template <int DT, int FORMAT, int DP, int RW, int WAVES, int KS = 1>
+template <int DT, int FORMAT, int DP, int RW, int WAVES, int KS = 1, bool TREE = false>
 struct Many {
     typedef mat<DT> M;
     typedef typename M::T T;
@@ -595,9 +624,11 @@ struct Many {
     static constexpr int KROW = DP * 2 + (WIDE ? 16 : 32), VROW = DP * 2 + (WIDE ? 64 : 32);
     static constexpr int BUF = TILE * (KROW + VROW) + TILE;     // keys, values, a byte for each key that is there
     static constexpr int LDS = 2 * BUF;
-    typedef Strays<DT, DP> St;
+    typedef Strays<DT, DP, TREE> St;
+    static __device__ __forceinline__ int32_t nodes_at(const Share& s) { return TREE ? s.last0 + 1 : 0; }
     static constexpr int SUFFIX_LDS = LDS + static_cast<int>(sizeof(St));
     static constexpr bool ONE = DP > 128;                       // one set of pieces on their way
+    static constexpr bool LATE = !CODES && DP == 128;           // a tree's masks are asked for where a tile holds nodes' keys: no register is left for them
 
     static __device__ __forceinline__ int key_of(int i) { return (THREADS / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
     static __device__ __forceinline__ int piece() { return static_cast<int>(threadIdx.x) % PIECES; }
@@ -671,7 +702,7 @@ struct Many {
         for (int key = key_of(0); key < TILE; key += THREADS / PIECES)
             if (key0 + key > sure_of(s))
 #pragma unroll 1
-                for (int h = 0; h < (CODES ? 2 : 1); ++h) reinterpret_cast<St*>(lds + LDS)->take_out(buf + TILE * KROW + key * VROW + 16 * (b + h), key0 + key, 8 * (b + h));
+                for (int h = 0; h < (CODES ? 2 : 1); ++h) reinterpret_cast<St*>(lds + LDS)->take_out(buf + TILE * KROW + key * VROW + 16 * (b + h), key0 + key - nodes_at(s), 8 * (b + h));
     }
 
     static __device__ __forceinline__ A mul(T8 a, T8 b, A c)
@@ -687,6 +718,8 @@ struct Many {
         // lane = row, and one of 2 (WIDE) or 4 groups of keys or elements
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
         const int part = wave / GROUPS * KEYS;                   // its keys of a tile
+        const int at_row = RW * (wave % GROUPS) + r;
+        const uint64_t nodes = TREE && !LATE ? nodes_of(a, s, at_row) : 0;
         T8 q[NC];
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = A{};
@@ -717,8 +750,8 @@ struct Many {
             const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane % TILE] != 0) & full_of(TILE);
             if (there != full_of(TILE) || key0 + TILE - 1 > s.last0) {
                 // this lane's keys, shifted so that each is a fixed bit (a mask made for every score would be held in registers)
-                const uint64_t mine = there >> (part + 4 * g);
-                const int32_t last = row.last - key0 - part - 4 * g;
+                const uint64_t mine = (TREE ? there & seen_from(s, LATE ? nodes_of(a, s, at_row) : nodes, key0) : there) >> (part + 4 * g);
+                const int32_t last = TREE ? TILE : row.last - key0 - part - 4 * g;
 #pragma unroll
                 for (int t = 0; t < NS; ++t)
 #pragma unroll
@@ -859,7 +892,7 @@ struct Many {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int i = 0; i < AN; ++i) o[t][i] += strays->of(RW * t + 8 * (i >> 2) + 4 * g + (i & 3), row.last);
+                for (int i = 0; i < AN; ++i) o[t][i] += strays->of(RW * t + 8 * (i >> 2) + 4 * g + (i & 3), row.last, TREE ? nodes_of(a, s, RW * group + r) : 0);
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
         float most = m == kNone ? kNone : m * a.c - kLift<DT>;
         if (!SUFFIX || !a.finish) {
