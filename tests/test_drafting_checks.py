@@ -142,7 +142,7 @@ def logits(x=P, stride=32000, out=2 * P, out_stride=32000, best=P, batch=4, node
     (dict(batch=1 << 24), SHAPE), (dict(nodes=65), SHAPE), (dict(nodes=65537, tree_masks=None, tree_tokens=None), SHAPE), (dict(lists=False), ARG),
     (dict(history_width=-1), SHAPE), (dict(history_width=1 << 20), SHAPE), (dict(biases=1024), SHAPE), (dict(biases=-1), SHAPE), (dict(x=None), ARG),
     (dict(history_lens=None), ARG), (dict(bias_tokens=None), ARG), (dict(bias_values=None), ARG), (dict(tree_tokens=None), ARG), (dict(tree_masks=None), ARG),
-    (dict(room=None), ARG), (dict(bytes_=12 * 8 * 4 - 1), ARG), (dict(x=P + 1), ALIGN), (dict(out=P + 1), ALIGN), (dict(best=P + 2), ALIGN), (dict(tree_masks=P + 4), ALIGN),
+    (dict(room=None, vocab=100000, out_stride=100000), ARG), (dict(bytes_=0, vocab=100000, out_stride=100000), ARG), (dict(x=P + 1), ALIGN), (dict(out=P + 1), ALIGN), (dict(best=P + 2), ALIGN), (dict(tree_masks=P + 4), ALIGN),
     (dict(history=P + 2), ALIGN), (dict(allowed=P + 2), ALIGN), (dict(room=P + 4), ALIGN), (dict(out_stride=31999), ARG), (dict(out=P, out_stride=40000), ARG),
     (dict(batch=0), B.OK), (dict(nodes=0), B.OK), (dict(out=None, best=None), B.OK),
 ])

@@ -163,6 +163,16 @@ def test_rows_beyond_32_bits():
     assert bool((x[:, 9] == -1).all()) and float(x[:, 10:].float().sum()) == 5.0
 
 
+def test_the_workspace_is_as_long_as_it_says():
+    c = build(3, 2, 100003, "bf16", biases=3, seed=4)
+    n = drafting.logits_workspace_bytes(3, 2, 100003, "bf16")
+    with pytest.raises(drafting.AddrmsError, match="workspace has"):
+        call(c, "bf16", 2, workspace=torch.empty(n - 8, dtype=torch.uint8, device="cuda"))
+    room = torch.full((n + 64,), 0xff, dtype=torch.uint8, device="cuda")
+    check(c, "bf16", 2, call(c, "bf16", 2, workspace=room[:n]))
+    assert (room[n:] == 0xff).all()
+
+
 def test_on_another_stream_and_in_a_graph():
     c = build(3, 4, 20011, "bf16", width=100, biases=20, masked=True, tree=True, seed=5)
     dev = {n: x.cuda() for n, x in c.items()}
@@ -176,8 +186,6 @@ def test_on_another_stream_and_in_a_graph():
     check(c, "bf16", 4, (out.cpu(), best.cpu()))
     with pytest.raises(ValueError, match="workspace"):
         drafting.logits_run(x, out, best, "bf16", nodes=4, **dev, stream=stream)
-    with pytest.raises(drafting.AddrmsError, match="workspace has"):
-        drafting.logits_run(x, out, best, "bf16", nodes=4, **dev, workspace=room[:-8])
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         drafting.logits_run(x, out, best, "bf16", nodes=4, **dev, workspace=room)
