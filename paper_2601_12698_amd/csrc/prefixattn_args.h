@@ -18,7 +18,10 @@ struct AttnArgs {
     int32_t finish;                                   // the suffixes' workgroups join the prefix's parts to their own, and write the output
     int32_t q_wide;                                   // queries can be read 16 bytes at a time
     float c;                                          // scale * log2(e): weights are powers of 2
-    uint64_t masks;                                   // of a tree's nodes (include/treeattn.h), whose keys follow suffix_lens
+    // Trees (treeattn.hip): masks of their nodes, whose keys follow suffix_lens; parts that the sequences' keys are cut into, together, but
+    // for one more of each; the shortest; and whether sequences come in the order of their lengths.
+    uint64_t masks;
+    int32_t cut_parts, cut_least, sorted;
 };
 
 // Forms of a workgroup: 16 rows whose four (FEW_8: eight) waves take keys in turn; 64, 128 or 256 rows that share their keys (64:

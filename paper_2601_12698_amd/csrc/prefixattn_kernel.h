@@ -538,10 +538,11 @@ struct Few {
             *reinterpret_cast<f32x4*>(join + (wave * ROWS + (lane & 15)) * OROW + 16 * t + 4 * g) = x;
         }
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
+        const int64_t each = TREE ? static_cast<int64_t>(a.q_len) * a.q_heads : rows;      // of a part: a sequence's, or all
         const float most = best == kNone ? kNone : best * a.c - kLift<DT>;
         const bool finish = SUFFIX && a.finish;
         if (!finish) {
-            if (wave == 0 && lane < 16 && row.in) at_global<float2>(a.part_ml)[s.part * rows + row.global] = make_float2(most, sum);
+            if (wave == 0 && lane < 16 && row.in) at_global<float2>(a.part_ml)[s.part * each + row.global] = make_float2(most, sum);
         } else {
             // the rows' weights of the prefix's parts: a wave takes rows in turn, its lanes the parts
             for (int r = wave; r < s.rows; r += WAVES) {
@@ -578,7 +579,7 @@ struct Few {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] += strays->of(e + j, row.last, TREE ? nodes_of(a, s, r) : 0);
             if (!finish) {
-                *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + (s.part * rows + global) * a.d + e) = x;
+                *reinterpret_cast<f32x4*>(at_global<float>(a.part_o) + (s.part * each + global) * a.d + e) = x;
                 continue;
             }
             x *= own[r];
@@ -623,12 +624,12 @@ struct Many {
     // the keys: a quarter of the LDS's time goes to conflicts, and 16 x 4 x 32 heads of 256 over 65536 fp16 keys take 260 us, not 249.)
     static constexpr int KROW = DP * 2 + (WIDE ? 16 : 32), VROW = DP * 2 + (WIDE ? 64 : 32);
     static constexpr int BUF = TILE * (KROW + VROW) + TILE;     // keys, values, a byte for each key that is there
-    static constexpr int LDS = 2 * BUF;
+    static constexpr int LDS = 2 * BUF + (TREE && !CODES && DP == 128 ? 8 * ROWS : 0);
     typedef Strays<DT, DP, TREE> St;
     static __device__ __forceinline__ int32_t nodes_at(const Share& s) { return TREE ? s.last0 + 1 : 0; }
     static constexpr int SUFFIX_LDS = LDS + static_cast<int>(sizeof(St));
     static constexpr bool ONE = DP > 128;                       // one set of pieces on their way
-    static constexpr bool LATE = !CODES && DP == 128;           // a tree's masks are asked for where a tile holds nodes' keys: no register is left for them
+    static constexpr bool LATE = !CODES && DP == 128;           // a tree's masks wait in LDS: no register is left for them
 
     static __device__ __forceinline__ int key_of(int i) { return (THREADS / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
     static __device__ __forceinline__ int piece() { return static_cast<int>(threadIdx.x) % PIECES; }
@@ -720,6 +721,8 @@ struct Many {
         const int part = wave / GROUPS * KEYS;                   // its keys of a tile
         const int at_row = RW * (wave % GROUPS) + r;
         const uint64_t nodes = TREE && !LATE ? nodes_of(a, s, at_row) : 0;
+        if constexpr (TREE && LATE)
+            if (static_cast<int>(threadIdx.x) < ROWS) *reinterpret_cast<uint64_t*>(lds + 2 * BUF + 8 * threadIdx.x) = nodes_of(a, s, threadIdx.x);
         T8 q[NC];
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] = A{};
@@ -750,7 +753,7 @@ struct Many {
             const uint64_t there = __ballot(buf[TILE * (KROW + VROW) + lane % TILE] != 0) & full_of(TILE);
             if (there != full_of(TILE) || key0 + TILE - 1 > s.last0) {
                 // this lane's keys, shifted so that each is a fixed bit (a mask made for every score would be held in registers)
-                const uint64_t mine = (TREE ? there & seen_from(s, LATE ? nodes_of(a, s, at_row) : nodes, key0) : there) >> (part + 4 * g);
+                const uint64_t mine = (TREE ? there & seen_from(s, LATE ? *reinterpret_cast<const uint64_t*>(lds + 2 * BUF + 8 * at_row) : nodes, key0) : there) >> (part + 4 * g);
                 const int32_t last = TREE ? TILE : row.last - key0 - part - 4 * g;
 #pragma unroll
                 for (int t = 0; t < NS; ++t)
@@ -847,20 +850,33 @@ struct Many {
     template <bool SUFFIX>
     __device__ __forceinline__ void run(const AttnArgs& a, const Share& s, char* lds)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
-        const int group = wave % GROUPS, part = wave / GROUPS * KEYS;      // its rows, and its keys of a tile
-        const Row row = row_of(a, s, RW * group + r);
-        const bool busy = RW * group < s.rows;                   // waves without rows only help to stage
         A o[NT];
         float m, l;
+        int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % RW, g = lane / RW;
+        int group = wave % GROUPS, part = wave / GROUPS * KEYS;  // its rows, and its keys of a tile
+        Row row = row_of(a, s, RW * group + r);
+        bool busy = RW * group < s.rows;                         // waves without rows only help to stage
         pass<false>(a, s, row, busy, lds, o, m, l);
+        const auto anew = [&] {                                  // not held in registers over a pass, where a tree leaves none
+            if constexpr (TREE) {
+                const int t = thread<true>();
+                lane = t & 63, wave = t >> 6, r = lane % RW, g = lane / RW;
+                group = wave % GROUPS, part = wave / GROUPS * KEYS;
+                row = row_of(a, s, RW * group + r);
+                busy = RW * group < s.rows;
+            }
+        };
+        anew();
         St* const strays = reinterpret_cast<St*>(lds + LDS);
         bool strayed = false;
         if (SUFFIX && sure_of(s) < kAll) {
             strays->look(o, wave, busy);
             __syncthreads();
             strayed = strays->template found<WAVES>();
-            if (__builtin_expect(strayed, 0)) pass<true>(a, s, row, busy, lds, o, m, l);
+            if (__builtin_expect(strayed, 0)) {
+                pass<true>(a, s, row, busy, lds, o, m, l);
+                anew();
+            }
         }
         if constexpr (KS == 2) {
             // what the waves of a tile's other half found, register by register
@@ -896,7 +912,7 @@ struct Many {
         const int64_t rows = static_cast<int64_t>(a.batch) * a.q_len * a.q_heads;
         float most = m == kNone ? kNone : m * a.c - kLift<DT>;
         if (!SUFFIX || !a.finish) {
-            const int64_t at = s.part * rows + row.global;
+            const int64_t at = s.part * (TREE ? static_cast<int64_t>(a.q_len) * a.q_heads : rows) + row.global;
             if (g == 0) at_global<float2>(a.part_ml)[at] = make_float2(most, l);
 #pragma unroll
             for (int t = 0; t < NT; ++t)

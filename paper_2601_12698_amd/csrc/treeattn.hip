@@ -1,11 +1,14 @@
 // Host side of attention of trees of drafted tokens (include/treeattn.h): argument checks, and how the work is split.
-#include "prefixattn_join.h"
+#include "treeattn_kernel.h"
+#include "prefixattn_plan.h"
 #include "treeattn.h"
 
 using namespace addrms_host;
 using namespace serving;
 
 namespace {
+
+constexpr int64_t kShort = 1024, kLong = 1 << 20;     // keys of a sequence, and bytes of a head's (see plan_of)
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
@@ -36,21 +39,49 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     }
     // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
     const bool prefix = a.prefix_len && a.pages, suffix = width && a.pages;
+    // Sequences of few keys: 16 rows a workgroup, whose waves share the keys, as often as there are rows; it reads the keys as often, but a
+    // form with more rows a workgroup goes over them tile by tile.  Whole calls of 32 query and 8 key heads of 128, us, so and with more rows:
+    //   8 x 16 nodes over 300 bf16 keys 10.8, 17.2      8 x 32 over 300 14.2, 22.7    2 x 16 over 700 11.4, 16.0     16 x 16 over 1000 23.6, 26.3
+    //   16 x 32 over 1000 e4m3 29.3, 32.5               4 x 16 over 1500 18.5, 16.3   32 x 16 over 2000 53.8, 45.3   64 x 16 over 500 51.8, 25.6
+    const int64_t units16 = tiles_of(own, FEW) * a.kv_heads * s->batch;
+    if (width <= kShort && units16 <= 2 * kFinishUnits) p->suffix_form = FEW;
     if (!prefix) p->prefix_form = p->suffix_form;
     a.prefix_tiles = static_cast<int32_t>(tiles_of(all, p->prefix_form));
     a.suffix_tiles = static_cast<int32_t>(tiles_of(own, p->suffix_form));
-    const int64_t prefix_units = static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, suffix_units = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads * s->batch;
-    a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, wanted(p->prefix_form), kMinChunk, &a.prefix_chunk) : 0;
-    p->finish = suffix && suffix_units >= kFinishUnits && a.prefix_splits <= kFinishSplits;
+    const int64_t prefix_units = static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, each = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads, suffix_units = each * s->batch;
+    auto split_prefix = [&](int64_t n) { a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, n, kMinChunk, &a.prefix_chunk) : 0; };
+    const int64_t slots = wanted(p->prefix_form), own_slots = wanted(p->suffix_form);
+    split_prefix(slots);
+    // Where the sequences fill the chip, a workgroup goes over all of a sequence's keys and joins the prefix's parts: no parts of the sequences'
+    // own (64 x 8 nodes over 1000 e4m3 keys 26.2 us in place of 38.7, 64 x 64 over 4096 bf16 338 in place of 465).  So also where one launch is
+    // all there is to few keys (8 nodes over 301 10.2, with two launches 10.8; over 700 13.6 and 11.6).  With few rows, whose parts are small,
+    // long sequences are cut until there are two workgroups a CU (40 sequences over 8000 e4m3 keys 90.6, cut 70.5; 64 x 2 over 4000 the same).
+    p->finish = suffix && a.prefix_splits <= kFinishSplits &&
+                (suffix_units >= (p->suffix_form == FEW && width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (p->suffix_form == FEW && width <= kShort / 2));
     if (p->finish && p->suffix_form == FEW) p->suffix_form = few(suffix_units);
     if (p->finish && !prefix) p->prefix_form = p->suffix_form;
     if (suffix) {
-        a.suffix_splits = splits_of(width, suffix_units, p->finish ? 1 : 2 * wanted(p->suffix_form), 2 * kMinChunk, &a.suffix_chunk);
-        p->suffix_blocks = round_up(a.kv_heads * static_cast<int64_t>(s->batch) * a.suffix_splits, 8) * a.suffix_tiles;
+        a.suffix_splits = 1;
+        if (!p->finish) {
+            // As many pieces as there are places, less one for the ends of sequences (1 x 32 nodes over 131072 e4m3 keys 96.8 us with 63 pieces of a
+            // head, 103.6 with 64, 111.5 with 96; 8 x 16 over 8191 34.8 with 62, 37.4 with 64, 45.4 with 128); more of them where many sequences end
+            // (40 over 8000: 76.9 with 62, 70.5 with 192).
+            a.cut_least = p->suffix_form == FEW ? kMinChunk : 2 * kMinChunk;
+            const int64_t most = std::min<int64_t>((width * s->batch + a.cut_least - 1) / a.cut_least, kMaxSplits - 1);
+            a.cut_parts = static_cast<int32_t>(std::clamp<int64_t>(std::max<int64_t>(own_slots / each - 1, 4 * s->batch), 1, most));
+            if (prefix) {
+                const int64_t own_blocks = std::min<int64_t>(a.cut_parts + s->batch, (width * s->batch + a.cut_least - 1) / a.cut_least) * each;
+                split_prefix(std::max(slots / 2, slots - own_blocks));
+            }
+        }
+        // the longest first where not all start at once (32 x 64 nodes over up to 4096 keys 170 us, in their order 214; where all start, 1.5 us are lost)
+        a.sorted = p->finish && s->batch <= 64 && suffix_units > own_slots;
+        p->suffix_blocks = round_up(a.kv_heads * (p->finish ? static_cast<int64_t>(s->batch) : a.cut_parts + static_cast<int64_t>(s->batch)), 8) * a.suffix_tiles;
     }
     p->prefix_blocks = round_up(static_cast<int64_t>(a.prefix_splits) * a.kv_heads, 8) * a.prefix_tiles;
-    const int64_t parts = a.prefix_splits + (p->finish ? 0 : a.suffix_splits);
-    p->bytes = parts * p->rows * (4ll * a.d + 8);
+    // parts of a sequence
+    const int64_t parts = static_cast<int64_t>(a.prefix_splits) * s->batch + (a.cut_parts ? a.cut_parts + static_cast<int64_t>(s->batch) : 0);
+    p->bytes = parts * s->q_len * s->q_heads * (4ll * a.d + 8);
     return fits(*p);
 }
 
@@ -101,7 +132,10 @@ int treeattn_run(const void* q, const int64_t* q_strides, const void* k_pages, c
         return ADDRMS_OK;
     }
     if (p.prefix_blocks + p.suffix_blocks) SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.prefix_blocks + p.suffix_blocks), s));
-    SERVING_HIP_TRY(launch_join<true>(p, shape->dtype, s));
+    const bool many = p.rows >= kJoinRows;
+    SERVING_HIP_TRY(launch_kernel(shape->dtype == ADDRMS_FP16 ? (many ? tree_join_kernel<DT_FP16, 1> : tree_join_kernel<DT_FP16, 4>)
+                                                              : (many ? tree_join_kernel<DT_BF16, 1> : tree_join_kernel<DT_BF16, 4>),
+                                  dim3(static_cast<unsigned>(many ? (p.rows + 3) / 4 : p.rows)), dim3(kJoinThreads), s, a));
     return ADDRMS_OK;
 }
 

@@ -5,6 +5,7 @@
 // shifted to the tile's first key and met with the keys that are there.
 #pragma once
 #include "prefixattn_kernel.h"
+#include "treeattn_cut.h"
 
 namespace serving {
 
@@ -47,16 +48,23 @@ __global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW 
     }
     if (threadIdx.x >= S::THREADS) return;                      // a form with more waves than the sequences' leaves the others idle
     b -= a.prefix_blocks;
-    const int32_t j = b >> 3, tile = j % a.suffix_tiles, unit = (j / a.suffix_tiles) * 8 + (b & 7);
-    const int32_t seq = unit / (a.suffix_splits * a.kv_heads);
-    if (seq >= a.batch) return;
-    const int32_t in_seq = unit - seq * a.suffix_splits * a.kv_heads, split = in_seq / a.kv_heads, room = a.suffix_width << a.page_shift;
-    s.head = in_seq - split * a.kv_heads;
+    const int32_t j = b >> 3, tile = j % a.suffix_tiles, unit = (j / a.suffix_tiles) * 8 + (b & 7), at = unit / a.kv_heads, room = a.suffix_width << a.page_shift;
+    s.head = unit - at * a.kv_heads;
+    int32_t seq = at, split = 0, piece = kAll;
+    if (a.cut_parts) {
+        const Piece p = piece_at(a, at);
+        if (p.seq < 0) return;
+        seq = p.seq, split = p.number, piece = p.keys;
+    } else {
+        if (at >= a.batch) return;
+        if (a.sorted) seq = by_length(a, at);
+    }
+    seq = __builtin_amdgcn_readfirstlane(seq), split = __builtin_amdgcn_readfirstlane(split), piece = __builtin_amdgcn_readfirstlane(piece);
     s.token0 = seq * a.q_len;
     s.row0 = tile * S::ROWS;
     s.rows = min(S::ROWS, a.q_len * a.group - s.row0);
-    s.part = a.prefix_splits + split;
-    s.first = split * a.suffix_chunk;
+    s.part = a.prefix_splits * a.batch + at - seq;
+    s.first = split * piece;
     s.table = a.suffix_pages + 4 * static_cast<int64_t>(seq) * a.suffix_width;
     const auto context = [&] { return min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), room); };
     if constexpr (SUFFIX == FEW || SUFFIX == FEW_8) {
@@ -70,16 +78,100 @@ __global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW 
         s.end = a.inline_len + room;
         const int32_t page0 = s.first < s.end ? S::page_of(a, s, s.first + S::TILE * (threadIdx.x >> 6), threadIdx.x & 63) : 0;
         const int32_t before = room ? context() : 0, keys = min(before + a.q_len, room);
-        s.end = a.inline_len ? a.inline_len + keys : min(s.first + a.suffix_chunk, keys);
+        s.end = a.inline_len ? a.inline_len + keys : min(piece < kAll ? s.first + piece : kAll, keys);
         s.last0 = a.inline_len + before - 1;
-        if (s.first >= s.end && !a.finish) return;              // the joining kernel knows the length, too
         S().template run<true>(a, s, page0, lds);
     } else {
         const int32_t before = context();
-        s.end = min(s.first + a.suffix_chunk, min(before + a.q_len, room));
+        s.end = min(piece < kAll ? s.first + piece : kAll, min(before + a.q_len, room));
         s.last0 = before - 1;
-        if (s.first >= s.end && !a.finish) return;
         S().template run<true>(a, s, lds);
+    }
+}
+
+// As prefixattn.hip's: out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, lse = ln 2 (m + log2 of that sum), over the prefix's parts and
+// those of the row's sequence.  WAVES waves join a row, lanes being columns of four elements by groups of parts.
+template <int DT, int WAVES>
+__global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(AttnArgs a)
+{
+    typedef typename elem<DT>::type T;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    constexpr int ROWS = kJoinThreads / 64 / WAVES, THREADS = 64 * WAVES, AHEAD = 4;
+    __shared__ float weight[ROWS][2 * kMaxSplits], red[2][4];
+    __shared__ f32x4 sums[kJoinThreads];
+    const int32_t tid = static_cast<int32_t>(threadIdx.x) % THREADS, slot = static_cast<int32_t>(threadIdx.x) / THREADS, wave = tid >> 6;
+    const int32_t each = a.q_len * a.q_heads, rows = a.batch * each;
+    const int32_t row = __builtin_amdgcn_readfirstlane(static_cast<int32_t>(blockIdx.x) * ROWS + slot);
+    if (row >= rows) return;                                    // with one wave a row: no barrier follows
+    const auto meet = [] {
+        if constexpr (WAVES > 1) __syncthreads();
+        else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    int32_t parts = a.prefix_splits;
+    int64_t own = 0;                                            // the row's place in its sequence's first part
+    if (a.cut_parts) {
+        const int32_t seq = row / each;
+        const Cut cut = cut_of(a, seq);
+        parts += cut.pieces;
+        own = (static_cast<int64_t>(a.prefix_splits) * a.batch + cut.before - seq) * each + row;
+    }
+    const auto place = [&](int32_t p) { return p < a.prefix_splits ? static_cast<int64_t>(p) * rows + row : own + static_cast<int64_t>(p - a.prefix_splits) * each; };
+    const int32_t cols = a.d / 4, groups = THREADS / cols, grp = tid / cols, col = tid - grp * cols;
+    const float* o = at_global<const float>(a.part_o) + 4 * col;
+    const int32_t mine = grp < groups && grp < parts ? (parts - grp + groups - 1) / groups : 0;      // parts that this lane adds
+    f32x4 first[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) first[i] = i < mine ? *reinterpret_cast<const f32x4*>(o + place(grp + i * groups) * a.d) : f32x4{0, 0, 0, 0};
+    const float2* ml = at_global<const float2>(a.part_ml);
+    float m = kNone;
+    for (int32_t p = tid; p < parts; p += THREADS) m = fmaxf(m, ml[place(p)].x);
+#pragma unroll
+    for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    if constexpr (WAVES > 1) {
+        if ((tid & 63) == 0) red[0][wave] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    }
+    float l = 0.0f;
+    for (int32_t p = tid; p < parts; p += THREADS) {
+        const float2 x = ml[place(p)];
+        // a part that saw no key has m = -inf, l = 0 and O = 0 (l is NaN where its scores were)
+        const float w = x.x == kNone ? 1.0f : __builtin_amdgcn_exp2f(x.x - m);
+        weight[slot][p] = w;
+        l += w * x.y;
+    }
+#pragma unroll
+    for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+    if constexpr (WAVES > 1) {
+        if ((tid & 63) == 0) red[1][wave] = l;
+    }
+    meet();
+    if constexpr (WAVES > 1) l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < mine) x += weight[slot][grp + i * groups] * first[i];
+    for (int32_t i = AHEAD; i < mine; i += AHEAD) {
+        f32x4 next[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) next[j] = *reinterpret_cast<const f32x4*>(o + place(grp + min(i + j, mine - 1) * groups) * a.d);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (i + j < mine) x += weight[slot][grp + (i + j) * groups] * next[j];
+    }
+    sums[threadIdx.x] = x;
+    meet();
+    if (grp == 0) {
+        for (int32_t g = 1; g < groups; ++g) x += sums[slot * THREADS + g * cols + col];
+        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;              // no key was seen: zeros
+        T4 y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = static_cast<T>(x[j] * inverse);
+        *reinterpret_cast<T4*>(at_global<T>(a.out) + static_cast<int64_t>(row) * a.d + 4 * col) = y;
+        if (a.lse && col == 0) at_global<float>(a.lse)[row] = lse_of(m, l);
     }
 }
 
