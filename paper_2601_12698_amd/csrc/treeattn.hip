@@ -24,27 +24,28 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     p->prefix_form = form_of(all, p->dp);
     auto wanted = [p](int form) { return form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
     auto few = [](int64_t units) { return units <= kFinishUnits ? FEW_8 : FEW; };
-    // a short prefix is seen by each sequence's workgroup, by prefixattn.hip's rule
-    const int64_t units = static_cast<int64_t>(a.kv_heads) * s->batch, key_bytes = std::max(256, 2 * p->dp * (s->format == KVCACHE_E4M3 ? 1 : 2));
-    const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
-    if (a.pages && a.prefix_len && p->suffix_form == FEW &&
-        (units >= kFinishUnits ? units * prefix_bytes <= kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain))) {
-        p->prefix_form = p->suffix_form = few(units);
-        p->finish = true;
-        a.inline_len = a.prefix_len;
-        a.suffix_tiles = a.suffix_splits = 1;
-        a.suffix_chunk = static_cast<int32_t>(width);
-        p->suffix_blocks = round_up(units, 8);
-        return fits(*p);
-    }
-    // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
-    const bool prefix = a.prefix_len && a.pages, suffix = width && a.pages;
     // Sequences of few keys: 16 rows a workgroup, whose waves share the keys, as often as there are rows; it reads the keys as often, but a
     // form with more rows a workgroup goes over them tile by tile.  Whole calls of 32 query and 8 key heads of 128, us, so and with more rows:
     //   8 x 16 nodes over 300 bf16 keys 10.8, 17.2      8 x 32 over 300 14.2, 22.7    2 x 16 over 700 11.4, 16.0     16 x 16 over 1000 23.6, 26.3
     //   16 x 32 over 1000 e4m3 29.3, 32.5               4 x 16 over 1500 18.5, 16.3   32 x 16 over 2000 53.8, 45.3   64 x 16 over 500 51.8, 25.6
     const int64_t units16 = tiles_of(own, FEW) * a.kv_heads * s->batch;
     if (width <= kShort && units16 <= 2 * kFinishUnits) p->suffix_form = FEW;
+    // a short prefix is seen by each sequence's workgroups, by prefixattn.hip's rule (16 x 7 nodes over 128 and up to 300 fp16 keys of 256 INLINE_A us,
+    // in two launches 29.8; over 600 and up to 300 INLINE_B and 35.0)
+    const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch, key_bytes = std::max(256, 2 * p->dp * (s->format == KVCACHE_E4M3 ? 1 : 2));
+    const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
+    if (a.pages && a.prefix_len && p->suffix_form == FEW &&
+        (units >= kFinishUnits ? units * prefix_bytes <= kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain))) {
+        p->prefix_form = p->suffix_form = few(units);
+        p->finish = true;
+        a.inline_len = a.prefix_len;
+        a.suffix_splits = 1;
+        a.suffix_tiles = static_cast<int32_t>(tiles_of(own, FEW));
+        p->suffix_blocks = round_up(a.kv_heads * static_cast<int64_t>(s->batch), 8) * a.suffix_tiles;
+        return fits(*p);
+    }
+    // a cache without a page has no key (the kernels read row 0 in the place of one that is not there)
+    const bool prefix = a.prefix_len && a.pages, suffix = width && a.pages;
     if (!prefix) p->prefix_form = p->suffix_form;
     a.prefix_tiles = static_cast<int32_t>(tiles_of(all, p->prefix_form));
     a.suffix_tiles = static_cast<int32_t>(tiles_of(own, p->suffix_form));
