@@ -601,7 +601,8 @@ struct Few {
     }
 };
 
-template <int DT, int FORMAT, int DP, int RW, int WAVES, int KS = 1, bool TREE = false>
+// TWO: a prefix is seen before a tree's sequence's own keys.
+template <int DT, int FORMAT, int DP, int RW, int WAVES, int KS = 1, bool TREE = false, bool TWO = false>
 struct Many {
     typedef mat<DT> M;
     typedef typename M::T T;
@@ -634,10 +635,22 @@ struct Many {
     static __device__ __forceinline__ int key_of(int i) { return (THREADS / PIECES) * i + static_cast<int>(threadIdx.x) / PIECES; }
     static __device__ __forceinline__ int piece() { return static_cast<int>(threadIdx.x) % PIECES; }
 
+    // The keys that a tile is of: their table of pages, the first one's number, and their end.  TWO: the prefix ends with a whole tile, those of
+    // its keys that are not there masked, so that a tile is of one table.  (A form of its own: this costs the others 1.5 %.)
+    struct From {
+        addr_t table;
+        int32_t base, end;
+    };
+    static __device__ __forceinline__ From from_of(const AttnArgs& a, const Share& s, int32_t key0)
+    {
+        if constexpr (TWO) return key0 >= s.turn ? From{s.table2, s.turn, s.end} : From{s.table, 0, a.inline_len};
+        else return From{s.table, 0, s.end};
+    }
     static __device__ __forceinline__ void pages_of(const AttnArgs& a, const Share& s, int32_t key0, int32_t (&page)[NP])
     {
+        const From from = from_of(a, s, key0);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) page[i] = at_global<const int32_t>(s.table)[min(key0 + key_of(i), s.end - 1) >> a.page_shift];
+        for (int i = 0; i < NP; ++i) page[i] = at_global<const int32_t>(from.table)[(min(key0 + key_of(i), from.end - 1) - from.base) >> a.page_shift];
     }
     // What a thread stages of a tile: pieces on their way from memory, then written to LDS as elements.
     struct Staged {
@@ -648,12 +661,13 @@ struct Many {
         __device__ __forceinline__ void load(const AttnArgs& a, const Share& s, int32_t key0, const int32_t (&page)[NP])
         {
             const int32_t row_bytes = a.d * ES, b = 16 * piece() < row_bytes ? 16 * piece() : 0;
+            const From from = from_of(a, s, key0);
             valid = 0;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const bool there = key0 + key_of(i) < s.end && in_cache(a, page[i]);
+                const bool there = key0 + key_of(i) < from.end && in_cache(a, page[i]);
                 valid |= there ? 1u << i : 0u;
-                const Place p = place_of(a, s.head, there ? page[i] : 0, key0 + key_of(i), row_bytes);
+                const Place p = place_of(a, s.head, there ? page[i] : 0, key0 + key_of(i) - from.base, row_bytes);
                 k[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.k_pages) + (p.bytes + b));
                 v[i] = *reinterpret_cast<const u32x4*>(at_global<const char>(a.v_pages) + (p.bytes + b));
                 if constexpr (CODES) {

@@ -30,17 +30,23 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     //   16 x 32 over 1000 e4m3 29.3, 32.5               4 x 16 over 1500 18.5, 16.3   32 x 16 over 2000 53.8, 45.3   64 x 16 over 500 51.8, 25.6
     const int64_t units16 = tiles_of(own, FEW) * a.kv_heads * s->batch;
     if (width <= kShort && units16 <= 2 * kFinishUnits) p->suffix_form = FEW;
-    // a short prefix is seen by each sequence's workgroups, by prefixattn.hip's rule (16 x 7 nodes over 128 and up to 300 fp16 keys of 256 INLINE_A us,
-    // in two launches 29.8; over 600 and up to 300 INLINE_B and 35.0)
+    // A short prefix is seen by each sequence's workgroups before its own keys, in one launch: with few rows by prefixattn.hip's rule, up to twice the
+    // bytes where they fill the chip (64 x 4 nodes over 700 and up to 100 bf16 keys 23.4 us, in two launches 29.4, 32 x 4 over 1400 21.0 and 26.3, over
+    // 64 x 1400 33.0 either way); with more rows, where that fills the chip, up to 16 keys for each row of a workgroup, for the work is the same and
+    // no part of the prefix's is written (64 x 64 nodes of 64 heads over 300 and up to 500 keys 141 us, so 219, over 2000 359 and 436; 64 x 32
+    // nodes of 32 heads over 300 43.7 and 60.3, over 2000 112 and 114, over 8000 349 and 304; 64 x 16 over 600 40.8 and 50.9, over 2000 76.5 and 73.6).
     const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch, key_bytes = std::max(256, 2 * p->dp * (s->format == KVCACHE_E4M3 ? 1 : 2));
     const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
-    if (a.pages && a.prefix_len && p->suffix_form == FEW &&
-        (units >= kFinishUnits ? units * prefix_bytes <= kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain))) {
-        p->prefix_form = p->suffix_form = few(units);
+    const bool together = p->suffix_form != FEW ? width && units >= kFinishUnits && a.prefix_len <= 16 * kFormRows[p->suffix_form]
+                          : units >= kFinishUnits ? units * prefix_bytes <= 2 * kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
+    if (a.pages && a.prefix_len && together) {
+        if (p->suffix_form == FEW) p->suffix_form = few(units);
+        p->prefix_form = p->suffix_form;
         p->finish = true;
         a.inline_len = a.prefix_len;
         a.suffix_splits = 1;
-        a.suffix_tiles = static_cast<int32_t>(tiles_of(own, FEW));
+        a.suffix_tiles = static_cast<int32_t>(tiles_of(own, p->suffix_form));
+        a.sorted = s->batch <= 64 && units > wanted(p->suffix_form);
         p->suffix_blocks = round_up(a.kv_heads * static_cast<int64_t>(s->batch), 8) * a.suffix_tiles;
         return fits(*p);
     }

@@ -9,21 +9,22 @@
 
 namespace serving {
 
-template <int DT, int FORMAT, int DP, int FORM, int WAVES> struct tree_form;
-template <int DT, int FORMAT, int DP, int WAVES> struct tree_form<DT, FORMAT, DP, FEW, WAVES> { typedef Few<DT, FORMAT, DP, WAVES, true> type; };
-template <int DT, int FORMAT, int DP, int WAVES> struct tree_form<DT, FORMAT, DP, FEW_8, WAVES> { typedef Few<DT, FORMAT, DP, 8, true> type; };
-template <int DT, int FORMAT, int DP, int WAVES> struct tree_form<DT, FORMAT, DP, MANY_64, WAVES> { typedef Many<DT, FORMAT, DP, 32, 4, 2, true> type; };
-template <int DT, int FORMAT, int DP, int WAVES> struct tree_form<DT, FORMAT, DP, MANY_128, WAVES> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4), 1, true> type; };
-template <int DT, int FORMAT, int DP, int WAVES> struct tree_form<DT, FORMAT, DP, MANY_256, WAVES> { typedef Many<DT, FORMAT, DP, 32, 8, 1, true> type; };
+template <int DT, int FORMAT, int DP, int FORM, int WAVES, bool TWO> struct tree_form;
+template <int DT, int FORMAT, int DP, int WAVES, bool TWO> struct tree_form<DT, FORMAT, DP, FEW, WAVES, TWO> { typedef Few<DT, FORMAT, DP, WAVES, true> type; };
+template <int DT, int FORMAT, int DP, int WAVES, bool TWO> struct tree_form<DT, FORMAT, DP, FEW_8, WAVES, TWO> { typedef Few<DT, FORMAT, DP, 8, true> type; };
+template <int DT, int FORMAT, int DP, int WAVES, bool TWO> struct tree_form<DT, FORMAT, DP, MANY_64, WAVES, TWO> { typedef Many<DT, FORMAT, DP, 32, 4, 2, true, TWO> type; };
+template <int DT, int FORMAT, int DP, int WAVES, bool TWO> struct tree_form<DT, FORMAT, DP, MANY_128, WAVES, TWO> { typedef Many<DT, FORMAT, DP, (DP > 128 ? 16 : 32), (DP > 128 ? 8 : 4), 1, true, TWO> type; };
+template <int DT, int FORMAT, int DP, int WAVES, bool TWO> struct tree_form<DT, FORMAT, DP, MANY_256, WAVES, TWO> { typedef Many<DT, FORMAT, DP, 32, 8, 1, true, TWO> type; };
 
 // Workgroups of the prefix first, then those of the sequences.  Workgroups go round the 8 XCDs; the row tiles of one head and
 // key range stand 8 apart, so that they read it through the same L2 at the same time.
-template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX>
+// TWO: the sequences' workgroups of many rows see the prefix first.  (Those of few rows may, in either case.)
+template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX, bool TWO>
 __global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW ? 1 : 2)) void tree_kernel(AttnArgs a)
 {
     constexpr int WAVES = threads_of(PREFIX, DP) / 64;          // few rows use all of them, whatever the prefix's form
     typedef typename form<DT, FORMAT, DP, PREFIX, WAVES>::type P;
-    typedef typename tree_form<DT, FORMAT, DP, SUFFIX, WAVES>::type S;
+    typedef typename tree_form<DT, FORMAT, DP, SUFFIX, WAVES, TWO>::type S;
     __shared__ __attribute__((aligned(16))) char lds[P::LDS > S::SUFFIX_LDS ? P::LDS : S::SUFFIX_LDS];
     int32_t b = static_cast<int32_t>(blockIdx.x);
     Share s;
@@ -67,24 +68,26 @@ __global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW 
     s.first = split * piece;
     s.table = a.suffix_pages + 4 * static_cast<int64_t>(seq) * a.suffix_width;
     const auto context = [&] { return min(max(at_global<const int32_t>(a.suffix_lens)[seq], 0), room); };
-    if constexpr (SUFFIX == FEW || SUFFIX == FEW_8) {
-        if (a.inline_len) {
-            s.table2 = s.table;
-            s.table = a.prefix_pages;
-            s.turn = a.inline_len;
-        }
+    constexpr bool MANY = SUFFIX != FEW && SUFFIX != FEW_8;
+    const int32_t shared = !MANY ? a.inline_len : TWO ? (a.inline_len + 63) / 64 * 64 : 0;        // where the sequence's own keys begin
+    if (shared) {
+        s.table2 = s.table;
+        s.table = a.prefix_pages;
+        s.turn = shared;
+    }
+    if constexpr (!MANY) {
         // The first tile's pages are asked for together with the length, as if the row of pages were full: a page number is checked
         // before it is used, and what is beyond the length masked.
-        s.end = a.inline_len + room;
+        s.end = shared + room;
         const int32_t page0 = s.first < s.end ? S::page_of(a, s, s.first + S::TILE * (threadIdx.x >> 6), threadIdx.x & 63) : 0;
         const int32_t before = room ? context() : 0, keys = min(before + a.q_len, room);
-        s.end = a.inline_len ? a.inline_len + keys : min(piece < kAll ? s.first + piece : kAll, keys);
-        s.last0 = a.inline_len + before - 1;
+        s.end = shared ? shared + keys : min(piece < kAll ? s.first + piece : kAll, keys);
+        s.last0 = shared + before - 1;
         S().template run<true>(a, s, page0, lds);
     } else {
-        const int32_t before = context();
-        s.end = min(piece < kAll ? s.first + piece : kAll, min(before + a.q_len, room));
-        s.last0 = before - 1;
+        const int32_t before = room ? context() : 0, keys = min(before + a.q_len, room);
+        s.end = shared ? shared + keys : min(piece < kAll ? s.first + piece : kAll, keys);
+        s.last0 = shared + before - 1;
         S().template run<true>(a, s, lds);
     }
 }

@@ -4,10 +4,10 @@
 namespace serving {
 namespace {
 
-template <int PREFIX, int SUFFIX>
+template <int PREFIX, int SUFFIX, bool TWO = false>
 hipError_t launch(const AttnArgs& a, unsigned blocks, hipStream_t s)
 {
-    return launch_kernel(tree_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX, SUFFIX>, dim3(blocks), dim3(threads_of(PREFIX, UNIT_DP)), s, a);
+    return launch_kernel(tree_kernel<UNIT_DT, UNIT_FORMAT, UNIT_DP, PREFIX, SUFFIX, TWO>, dim3(blocks), dim3(threads_of(PREFIX, UNIT_DP)), s, a);
 }
 
 }  // namespace
@@ -17,6 +17,14 @@ hipError_t TREE_UNIT(UNIT_DT, UNIT_FORMAT, UNIT_DP)(const AttnArgs& a, int prefi
 {
     if (prefix_form == FEW_8) return launch<FEW_8, FEW_8>(a, blocks, s);
     if (prefix_form == FEW) return launch<FEW, FEW>(a, blocks, s);
+    if (a.inline_len) {
+        if constexpr (UNIT_DP <= 128)
+            if (suffix_form == MANY_64) return launch<MANY_64, MANY_64, true>(a, blocks, s);
+#if UNIT_DP == 128
+        if (suffix_form == MANY_256) return launch<MANY_256, MANY_256, true>(a, blocks, s);
+#endif
+        return launch<MANY_128, MANY_128, true>(a, blocks, s);
+    }
     if constexpr (UNIT_DP <= 128) {
         if (prefix_form == MANY_64) return suffix_form == FEW ? launch<MANY_64, FEW>(a, blocks, s) : launch<MANY_64, MANY_64>(a, blocks, s);
         if (prefix_form == MANY_128 && suffix_form == MANY_64) return launch<MANY_128, MANY_64>(a, blocks, s);

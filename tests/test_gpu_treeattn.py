@@ -126,6 +126,17 @@ CASES = [
     (64, 25, 24, 4, 128, 65, [(13 * i) % 90 for i in range(64)], 8, 16, "bf16", True),
     (86, 20, 21, 3, 64, 200, [(7 * i) % 60 for i in range(86)], 6, 16, "fp16", True),
     (64, 64, 20, 4, 128, 0, [(29 * i) % 200 for i in range(64)], 5, 64, "bf16", False),
+    # the same with a prefix that the sequences' workgroups see before their own keys, in tiles of its own
+    (64, 16, 16, 4, 128, 130, [(7 * i) % 50 for i in range(64)], 5, 16, "bf16", False),
+    (64, 16, 16, 4, 64, 64, [(7 * i) % 50 for i in range(64)], 5, 16, "fp16", True),
+    (64, 30, 16, 4, 112, 63, [(5 * i) % 70 for i in range(64)], 7, 16, "fp16", False),
+    (130, 10, 16, 2, 256, 70, [(3 * i) % 30 for i in range(130)], 3, 16, "bf16", True),
+    (130, 10, 16, 2, 256, 200, [(3 * i) % 30 for i in range(130)], 5, 8, "fp16", False),
+    (64, 40, 20, 4, 128, 700, [(9 * i) % 100 for i in range(64)], 5, 32, "bf16", True),
+    # a prefix and nothing else
+    (64, 40, 20, 4, 128, 300, [], 0, 32, "bf16", True),
+    (64, 3, 8, 4, 128, 100, [], 0, 32, "fp16", False),
+    (2, 10, 8, 2, 256, 40, [], 0, 8, "bf16", False),
 ]
 name = lambda c: "x".join(str(x) for x in c[:6]) + f"_{c[8]}_{c[9]}_{'e4m3' if c[10] else 'same'}"  # noqa: E731
 
