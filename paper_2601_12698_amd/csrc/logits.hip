@@ -108,8 +108,9 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
 
     struct Row {
         typename V::type x[PIECES];
-        uint32_t bits;                                          // tokens that the grammar allows
+        uint32_t word[PIECES];                                  // the mask's, of each piece
     };
+    // Nothing here looks at what it loads: it may be under way for long.
     const auto load = [&](Row& to, uint32_t i) {
         const uint32_t row = seq * a.nodes + i;
         if (n >= N) {
@@ -120,20 +121,15 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
                 to.x[k] = *reinterpret_cast<const typename V::loose*>(x + (e + N <= n ? e : 0));
             }
         }
-        to.bits = ~0u;
         if (a.allowed) {
             const uint32_t* allowed = at_global<const uint32_t>(a.allowed) + row * a.allowed_stride + v0 / 32;
-            uint32_t word[PIECES];
 #pragma unroll
-            for (uint32_t k = 0; k < PIECES; ++k) word[k] = allowed[min(N * (tid + k * THREADS), n - 1) / 32];
-            to.bits = 0;
-#pragma unroll
-            for (uint32_t k = 0; k < PIECES; ++k) to.bits |= (word[k] >> (N * tid % 32) & kPiece) << (N * k);        // N * THREADS is a multiple of 32
+            for (uint32_t k = 0; k < PIECES; ++k) to.word[k] = allowed[min(N * (tid + k * THREADS), n - 1) / 32];
         }
     };
 
     Row now, next;
-    load(now, first);
+    if constexpr (!LISTS) load(now, first);
     float r = 1.0f, f = 0.0f, p = 0.0f;
     int32_t node_token = -1;
     const bool tree = LISTS && a.tree_masks && a.penalties;
@@ -166,6 +162,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
             r = pen[0], f = pen[1], p = pen[2];
         }
         if (a.tree_masks && tid < a.nodes) node_token = at_global<const int32_t>(a.tree_tokens)[seq * a.nodes + tid];
+        load(now, first);                                       // loads come back in their order: while these do, the lists are taken in
 #pragma unroll
         for (uint32_t i = 4 * tid; i < CHUNK; i += 4 * THREADS) *reinterpret_cast<u32x4*>(words + i) = u32x4{0, 0, 0, 0};
         if constexpr (!BUILD) named_in[tid] = 0;
@@ -174,8 +171,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
         if (a.history) {
             len = min(max(len, 0), static_cast<int32_t>(a.history_width));
             prompt = min(max(prompt, 0), len);
-#pragma unroll 1
-            for (int32_t from = 0; from < len; from += BATCH * THREADS) {
+            const auto take = [&](int32_t from) {               // the batch from here on, while the next one is under way
                 int32_t here[BATCH];
 #pragma unroll
                 for (uint32_t k = 0; k < BATCH; ++k) here[k] = batch[k];
@@ -190,7 +186,10 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
                         if constexpr (!BUILD) name(t);
                     }
                 }
-            }
+            };
+            take(0);                                            // apart, so that it waits for its own loads and not for the row's behind them
+#pragma unroll 1
+            for (int32_t from = BATCH * THREADS; from < len; from += BATCH * THREADS) take(from);
         }
         if (a.biases) {
             __syncthreads();
@@ -243,6 +242,12 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
 #pragma unroll 1
     for (uint32_t i = first; i < last; ++i) {
         const uint32_t row = seq * a.nodes + i;
+        uint32_t bits = ~0u;                                    // tokens that the grammar allows
+        if (a.allowed) {
+            bits = 0;
+#pragma unroll
+            for (uint32_t k = 0; k < PIECES; ++k) bits |= __builtin_amdgcn_ubfe(now.word[k], N * tid % 32, N) << (N * k);        // N * THREADS is a multiple of 32
+        }
         if constexpr (LISTS)
             if (tree) {
                 const uint32_t t = static_cast<uint32_t>(node_token) - v0;
@@ -257,8 +262,8 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
         if (tree && i + 1 < last) path = at_global<const uint64_t>(a.tree_masks)[row + 1];
         T* const y = at_global<T>(a.out) + row * a.out_stride + v0;
         uint32_t left = edge;                                   // tokens that are taken one by one
-        if constexpr (LISTS) left |= named_in[tid] & now.bits & have;
-        const uint32_t same = now.bits & have & ~left;          // tokens that stay what they are
+        if constexpr (LISTS) left |= named_in[tid] & bits & have;
+        const uint32_t same = bits & have & ~left;          // tokens that stay what they are
         float top = -__builtin_huge_valf();
         uint32_t piece = 0;                                     // that the best so far is in
 #pragma unroll
@@ -280,8 +285,8 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
 #pragma unroll
                     for (uint32_t w = 0; w < 4; ++w) {
                         // -infinity in the place of what is ruled out
-                        const uint32_t in = N == 4 ? spread(now.bits, N * k + w)
-                                                   : (spread(now.bits, N * k + 2 * w) & 0xffffu) | (spread(now.bits, N * k + 2 * w + 1) & 0xffff0000u);
+                        const uint32_t in = N == 4 ? spread(bits, N * k + w)
+                                                   : (spread(bits, N * k + 2 * w) & 0xffffu) | (spread(bits, N * k + 2 * w + 1) & 0xffff0000u);
                         constexpr uint32_t low = DT == DT_FP32 ? 0xff800000u : DT == DT_BF16 ? 0xff80ff80u : 0xfc00fc00u;
                         kept[w] = (kept[w] & in) | (low & ~in);
                     }
@@ -318,7 +323,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
             float z;
             if constexpr (DT == DT_FP32) z = __builtin_bit_cast(float, word);
             else z = static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(j & 1 ? word >> 16 : word)));
-            if (edge >> b & 1) z = now.bits >> b & 1 ? static_cast<float>((at_global<const T>(a.logits) + row * a.logits_stride + v0)[e]) : -__builtin_huge_valf();
+            if (edge >> b & 1) z = bits >> b & 1 ? static_cast<float>((at_global<const T>(a.logits) + row * a.logits_stride + v0)[e]) : -__builtin_huge_valf();
             if constexpr (LISTS) {
                 const uint32_t w = words[e];
                 if (w & (kMet | kMade)) z = z > 0.0f ? z / r : z * r;
@@ -327,7 +332,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
                     z = z - p;
                 }
                 if (w & kBias) z = z + sums[LOGITS_MAX_BIASES - ((w & kBias) >> 21)];
-                if (!(now.bits >> b & 1)) z = -__builtin_huge_valf();
+                if (!(bits >> b & 1)) z = -__builtin_huge_valf();
             }
             mine.take(order_of(z), ~(v0 + e));
             if (a.out) y[e] = static_cast<T>(z);
