@@ -433,7 +433,7 @@ int logits_run(const void* logits, int64_t logits_stride, void* out, int64_t out
     if (!out && !best) return ADDRMS_OK;
     LogitsArgs a = {};
     a.logits = addr(logits), a.out = addr(out), a.best = addr(best), a.penalties = addr(l.penalties);
-    a.history = l.history_width ? addr(l.history) : 0, a.history_lens = addr(l.history_lens), a.prompt_lens = addr(l.prompt_lens);
+    a.history = l.penalties && l.history_width ? addr(l.history) : 0, a.history_lens = addr(l.history_lens), a.prompt_lens = addr(l.prompt_lens);
     a.bias_tokens = addr(l.bias_tokens), a.bias_values = addr(l.bias_values), a.allowed = addr(l.allowed);
     a.tree_tokens = addr(l.tree_tokens), a.tree_masks = addr(l.tree_masks), a.partial = addr(workspace);
     a.logits_stride = logits_stride, a.out_stride = out_stride, a.history_stride = l.history_stride, a.allowed_stride = l.allowed_stride;

@@ -142,6 +142,21 @@ def test_lengths_beyond_the_lists_and_tokens_that_are_none():
     check(c, "fp32", 1, call(c, "fp32", 1))
 
 
+@pytest.mark.parametrize("vocab", [500, 40001])
+def test_lists_that_say_nothing_and_rows_that_share_theirs(vocab):
+    """Histories without penalties; penalties without histories; one history and one mask for all rows, by a stride of 0."""
+    c = build(4, 1, vocab, "bf16", width=60, biases=5, masked=True, seed=6)
+    for leave in (("penalties",), ("history", "history_lens", "prompt_lens"), ("bias_tokens", "bias_values"), ("allowed", "penalties")):
+        some = {n: x for n, x in c.items() if n not in leave}
+        check(some, "bf16", 1, call(some, "bf16", 1))
+    dev = {n: x.cuda() for n, x in c.items()}
+    x = dev.pop("logits")
+    dev["history"], dev["allowed"] = dev["history"][:1].expand(4, -1), dev["allowed"][:1].expand(4, -1)
+    out, best = torch.empty_like(x), torch.empty(4, dtype=torch.int32, device="cuda")
+    drafting.logits_run(x, out, best, "bf16", **dev)
+    check(dict(c, history=c["history"][:1].expand(4, -1), allowed=c["allowed"][:1].expand(4, -1)), "bf16", 1, (out.cpu(), best.cpu()))
+
+
 def test_a_token_that_fills_its_history():
     """Counts of hundreds of thousands: as many as a history may hold."""
     n = drafting.MAX_HISTORY

@@ -2,6 +2,7 @@
 general ones (needs an MI355X)."""
 import importlib.util
 import os
+import sys
 
 import pytest
 import torch
@@ -28,6 +29,14 @@ def test_the_tree():
     for i, p in enumerate(e.PARENTS):
         assert masks[i] == (0 if p < 0 else masks[p]) | 1 << i and p < i
     assert len({(p, g) for p, g in zip(e.PARENTS, e.GUESS)}) == len(masks)           # no two children have one guess
+
+
+@pytest.mark.parametrize("args", [["--steps", "0"], ["--steps", "-3", "--check"], ["--batch", "0"], ["--prompt", "0"]])
+def test_nothing_to_do_is_refused(args, monkeypatch, capsys):
+    monkeypatch.setattr(sys, "argv", ["tree_decode.py", *args])
+    with pytest.raises(SystemExit) as e:
+        example().main()
+    assert e.value.code == 2 and "at least 1" in capsys.readouterr().err
 
 
 @pytest.mark.gpu

@@ -133,6 +133,8 @@ CASES = [
     (130, 10, 16, 2, 256, 70, [(3 * i) % 30 for i in range(130)], 3, 16, "bf16", True),
     (130, 10, 16, 2, 256, 200, [(3 * i) % 30 for i in range(130)], 5, 8, "fp16", False),
     (64, 40, 20, 4, 128, 700, [(9 * i) % 100 for i in range(64)], 5, 32, "bf16", True),
+    # many sequences beside a prefix in more parts than a sequence's workgroup joins
+    (300, 1, 1, 1, 64, 9000, [(5 * i) % 14 for i in range(300)], 2, 8, "bf16", False),
     # a prefix and nothing else
     (64, 40, 20, 4, 128, 300, [], 0, 32, "bf16", True),
     (64, 3, 8, 4, 128, 100, [], 0, 32, "fp16", False),
