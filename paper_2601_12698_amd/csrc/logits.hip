@@ -6,6 +6,8 @@
 // Bound by memory where rows are many: 8 x 24 x 131072 bf16 without lists 21 us a call, with out alone 15.7 (6.6 TB/s); the lists of 16384
 // tokens take 12 more, most of it the named tokens (a quarter of all), whose division and places are some 60 instructions a turn.
 // Small calls are bound by fetching code: 1 x 32000 bf16 took 11.4 us with 24 KB of it and takes 7.8 with 8.
+#include <algorithm>
+
 #include "logits.h"
 #include "serving_internal.h"
 
@@ -14,7 +16,8 @@ using namespace serving;
 
 namespace {
 
-constexpr int kThreads = 256, kManyThreads = 1024;
+constexpr int kThreads = 256, kLongThreads = 512, kManyThreads = 1024;
+constexpr int32_t kLongHistory = 8192;        // tokens
 constexpr uint32_t kEach = 32;                // tokens of a thread: a bit each
 // A token's word: whether the prompt has it, the first bias that names it (counted down from 1023), how often it was made.
 constexpr uint32_t kMet = 1u << 31, kMade = (1u << 21) - 1, kBias = LOGITS_MAX_BIASES << 21;
@@ -82,11 +85,11 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
 {
     typedef Vec<DT> V;
     typedef typename V::T T;
-    constexpr uint32_t N = V::N, CHUNK = kEach * THREADS, PIECES = kEach / N, NAMED = (LOGITS_MAX_BIASES + THREADS - 1) / THREADS, BATCH = THREADS == kThreads ? 16 : 4, WAVES = THREADS / 64;
+    constexpr uint32_t N = V::N, CHUNK = kEach * THREADS, PIECES = kEach / N, NAMED = (LOGITS_MAX_BIASES + THREADS - 1) / THREADS, BATCH = THREADS < kManyThreads ? 16 : 4, WAVES = THREADS / 64;
     constexpr uint32_t kPiece = (1u << N) - 1;
     // Which tokens are named is seen from their words where a workgroup takes in long lists (8 x 24 x 131072 34.6 us, so 33.6), else noted
     // with each (1 x 32000 8.6 us, so 8.0).
-    constexpr bool BUILD = THREADS == kThreads;
+    constexpr bool BUILD = THREADS < kManyThreads;
     constexpr bool AHEAD = DT != DT_FP32;                       // the next row is under way; two of fp32 would leave fewer waves on a CU
     __shared__ __attribute__((aligned(16))) uint32_t words[LISTS ? CHUNK : 4];
     __shared__ float sums[LISTS ? LOGITS_MAX_BIASES : 1];
@@ -384,8 +387,12 @@ int check(int64_t batch, int32_t nodes, int64_t vocab, int dtype)
 // (1 x 32000 bf16 7.8 us, with 256 threads 8.8; 256 x 32000 10.9 and 14.4; 32 x 16 nodes x 32000 18.4 and 20.1).  Of longer rows they have
 // a quarter as many lists to go over, but come one a CU: 8 x 24 nodes x 131072 with histories of up to 16384 31.3 us in place of 33.3, but 8
 // x 40000 10.0 in place of 9.1, 256 x 50001 23.7 in place of 22.5, 8 x 24 x 100000 fp32 38.2 in place of 33.4, 16 x 8 x 152000 22.9 and 19.5.
-int threads_of(int64_t vocab) { return vocab <= kEach * kManyThreads ? kManyThreads : kThreads; }
-int64_t chunks_of(int64_t vocab) { return (vocab + kEach * threads_of(vocab) - 1) / (kEach * threads_of(vocab)); }
+// Of the others, long histories are gone over half as often by 512 threads (8 x 24 x 131072 with up to 16384 32.4 us in place of 33.3, 1 x 64 nodes x
+// 50001 with 30000 18.4 and 23.1), short ones are not worth it (256 x 50001 24.9 in place of 22.4).
+int threads_of(int64_t vocab, int32_t history) { return vocab <= kEach * kManyThreads ? kManyThreads : history >= kLongHistory ? kLongThreads : kThreads; }
+int64_t chunks_of(int64_t vocab, int threads) { return (vocab + kEach * threads - 1) / (kEach * threads); }
+// Partial results of a row: one of each wave, none where one workgroup has the row.
+int64_t partials_of(int64_t vocab, int threads) { return chunks_of(vocab, threads) > 1 ? chunks_of(vocab, threads) * (threads / 64) : 0; }
 
 }  // namespace
 
@@ -394,7 +401,7 @@ extern "C" {
 int64_t logits_workspace_bytes(int64_t batch, int32_t nodes, int64_t vocab, int dtype)
 {
     if (const int st = check(batch, nodes, vocab, dtype)) return st;
-    return chunks_of(vocab) > 1 ? 8 * batch * nodes * chunks_of(vocab) * (threads_of(vocab) / 64) : 0;
+    return vocab <= kEach * kManyThreads ? 0 : 8 * batch * nodes * std::max(partials_of(vocab, kThreads), partials_of(vocab, kLongThreads));
 }
 
 int64_t logits_algorithmic_bytes(int64_t batch, int32_t nodes, int64_t vocab, int dtype, int64_t tokens, int32_t biases, int masked, int write)
@@ -439,13 +446,13 @@ int logits_run(const void* logits, int64_t logits_stride, void* out, int64_t out
     a.logits_stride = logits_stride, a.out_stride = out_stride, a.history_stride = l.history_stride, a.allowed_stride = l.allowed_stride;
     a.vocab = static_cast<uint32_t>(vocab), a.nodes = static_cast<uint32_t>(nodes), a.rows = static_cast<uint32_t>(batch * nodes);
     a.biases = static_cast<uint32_t>(l.biases), a.history_width = static_cast<uint32_t>(l.history_width);
-    const int threads = threads_of(vocab);
-    a.chunks = static_cast<uint32_t>(chunks_of(vocab));
-    a.partials = a.chunks * threads / 64;
+    const int threads = threads_of(vocab, a.history ? l.history_width : 0);
+    a.chunks = static_cast<uint32_t>(chunks_of(vocab, threads));
+    a.partials = static_cast<uint32_t>(partials_of(vocab, threads));
     const bool used = l.biases || (l.penalties && (a.history || l.tree_masks));
     // A tree's rows are shared out until the chip is full twice over, or with one workgroup a CU full; each share takes in the lists anew (8
     // x 24 nodes x 131072 with 256 threads: 52.6 us with 256 workgroups, 35.8 with 512, 33.3 with 1024, 36.7 with 2048).
-    const int64_t wanted = threads == kThreads ? 1024 : 256, units = a.chunks * batch;
+    const int64_t wanted = threads == kThreads ? 1024 : threads == kLongThreads ? 512 : 256, units = a.chunks * batch;
     int64_t parts = used ? (wanted + units - 1) / units : nodes;
     if (parts > nodes) parts = nodes;
     a.part_rows = static_cast<uint32_t>((nodes + parts - 1) / parts);
@@ -453,10 +460,11 @@ int logits_run(const void* logits, int64_t logits_stride, void* out, int64_t out
     if (!launchable(units * a.parts, threads)) return fail(ADDRMS_ERR_UNSUPPORTED_SHAPE, "the call is too large: %lld workgroups", (long long)(units * a.parts));
     const dim3 grid(static_cast<unsigned>(units * a.parts));
     const hipStream_t s = static_cast<hipStream_t>(stream);
-#define GO(DT) launch_kernel(threads == kThreads ? (used ? logits_kernel<DT, true, kThreads> : logits_kernel<DT, false, kThreads>) \
-                                                 : (used ? logits_kernel<DT, true, kManyThreads> : logits_kernel<DT, false, kManyThreads>), grid, dim3(threads), s, a)
+#define AS(DT, T) launch_kernel(used ? logits_kernel<DT, true, T> : logits_kernel<DT, false, T>, grid, dim3(threads), s, a)
+#define GO(DT) (threads == kThreads ? AS(DT, kThreads) : threads == kLongThreads ? AS(DT, kLongThreads) : AS(DT, kManyThreads))
     SERVING_HIP_TRY(dtype == ADDRMS_BF16 ? GO(DT_BF16) : dtype == ADDRMS_FP16 ? GO(DT_FP16) : GO(DT_FP32));
 #undef GO
+#undef AS
     if (best && a.chunks > 1)
         SERVING_HIP_TRY(launch_kernel(best_kernel, dim3(static_cast<unsigned>((a.rows + kThreads / 64 - 1) / (kThreads / 64))), dim3(kThreads), s, a));
     return ADDRMS_OK;

@@ -82,13 +82,14 @@ def test_trees_without_work_and_unknown_shapes():
 
 
 def test_tree_workspace_holds_a_part_for_each_split():
-    """4 d + 8 bytes for each row and part, never more parts than pieces of 128 keys."""
+    """4 d + 8 bytes for each row and part: of the prefix never more parts than pieces of 128 keys, of the sequences together no more than
+    such pieces and one for the end of each."""
     for prefix, width in ((0, 4), (256, 0), (257, 40), (100000, 100), (0, 1 << 13)):
         for batch, nodes, heads in ((1, 1, (1, 1)), (64, 64, (64, 8)), (3, 40, (8, 2)), (1, 64, (32, 8))):
             s = shape(batch=batch, q_len=nodes, q_heads=heads[0], kv_heads=heads[1], prefix_len=prefix, suffix_width=width, pages=1 << 20)
-            rows, n = batch * nodes * heads[0], D.treeattn_workspace_bytes(s)
-            assert n % (rows * (4 * 128 + 8)) == 0
-            assert n // (rows * (4 * 128 + 8)) <= -(-prefix // 128) + -(-width * 16 // 128)
+            part, n = nodes * heads[0] * (4 * 128 + 8), D.treeattn_workspace_bytes(s)       # of one sequence
+            assert n % part == 0
+            assert n // part <= batch * -(-prefix // 128) + -(-batch * width * 16 // 128) + (batch if width else 0)
 
 
 def accept(chosen=P, tokens=P, masks=P, table=P, lens=P, path=P, count=P, follows=P, f=P, t=P, batch=4, nodes=8, depth=5, width=10, pages=100, page=16):
