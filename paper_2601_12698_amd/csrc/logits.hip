@@ -3,8 +3,8 @@
 // A workgroup has a chunk of the vocabulary and some of a sequence's rows.  What the sequence's lists say of the chunk's tokens is
 // gathered in LDS once, a word a token; then the rows pass by, each logit read once and written once.  Few tokens are named by a list:
 // the others stay what they are but for the mask, without arithmetic, and the named ones are taken one by one by the thread that has them.
-// Bound by memory where rows are many: 8 x 24 x 131072 bf16 without lists 21 us a call, with out alone 15.7 (6.6 TB/s); the lists of 16384
-// tokens take 12 more, most of it the named tokens (a quarter of all), whose division and places are some 60 instructions a turn.
+// Bound by memory where rows are many: 8 x 24 x 131072 bf16 without lists 20.6 us a call, with out alone 15.7 (6.6 TB/s); lists of up to 16384
+// tokens take 12 more, most of it the named tokens (some hundreds of a chunk's), whose places and division are some 60 instructions a turn.
 // Small calls are bound by fetching code: 1 x 32000 bf16 took 11.4 us with 24 KB of it and takes 7.8 with 8.
 #include <algorithm>
 
@@ -310,10 +310,11 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a)
             mine.order = have ? order_of(top) : 0;
             if (mine.order == most_of_wave(mine.order)) {
                 const typename V::type x = __builtin_bit_cast(typename V::type, piece_of(piece));
-                uint32_t e = 0;                                 // where all are ruled out or -infinity: the first
+                uint32_t e = 0;
 #pragma unroll
                 for (uint32_t j = N; j-- > 0;)
                     if ((same >> (N * piece + j) & 1) && order_of(static_cast<float>(x[j])) == mine.order) e = j;
+                if (top == -__builtin_huge_valf()) e = 0;       // nothing is above what is ruled out: the first, also where it is that
                 mine.down = ~(v0 + N * (tid + piece * THREADS) + e);
             }
         }

@@ -134,6 +134,27 @@ def test_best_of_ties_nan_infinities_and_rows_without_a_token(vocab):
         check(lists, dtype, 1, call(lists, dtype, 1))
 
 
+@pytest.mark.parametrize("vocab", [31, 8200, 70000])
+def test_best_where_all_that_is_allowed_is_minus_infinity(vocab):
+    """What is ruled out is -infinity as well: the lowest token, not the lowest that is allowed."""
+    x = torch.full((4, vocab), 2.0)
+    x[0, 5] = x[0, vocab - 1] = x[1, vocab - 2] = -math.inf
+    x[2, 7:] = -math.inf
+    x[3, 11] = -1e30
+    allowed = torch.zeros((4, -(-vocab // 32)), dtype=torch.int32)
+    for row, t in ((0, 5), (0, vocab - 1), (1, vocab - 2), (2, 7), (2, 9), (2, 13), (3, 11)):
+        allowed[row, t // 32] |= -2 ** 31 if t % 32 == 31 else 1 << t % 32
+    for dtype in ("bf16", "fp32"):
+        c = {"logits": x.to(R.TYPES[dtype]), "allowed": allowed}
+        got = call(c, dtype, 1)
+        check(c, dtype, 1, got)
+        assert got[1].tolist() == [0, 0, 0, 11]
+        lists = dict(c, penalties=torch.tensor([[1.5, 0.5, 0.5]] * 4), history=torch.tensor([[5], [3], [9], [0]], dtype=torch.int32), history_lens=torch.ones(4, dtype=torch.int32))
+        got = call(lists, dtype, 1)
+        check(lists, dtype, 1, got)
+        assert got[1].tolist() == [0, 0, 0, 11]
+
+
 def test_lengths_beyond_the_lists_and_tokens_that_are_none():
     c = build(4, 1, 300, "fp32", width=20, seed=2)
     c["history_lens"] = torch.tensor([2 ** 31 - 1, -5, 20, 3], dtype=torch.int32)
