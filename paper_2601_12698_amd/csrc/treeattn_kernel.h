@@ -1,8 +1,12 @@
 // Device side of attention of trees of drafted tokens (include/treeattn.h).
 //
 // A sequence's nodes are its rows, as in prefixattn_kernel.h, whose two forms of a workgroup are used here: the keys below the tree
-// are seen by all rows, so that only a tile that holds nodes' keys (the last, or the last two) looks at masks, a row's 64 bits
+// are seen by all rows, so that only a tile that holds nodes' keys (of the last two or three) looks at masks, a row's 64 bits
 // shifted to the tile's first key and met with the keys that are there.
+//
+// Many rows are bound by matrix instructions and the softmax between them (64 x 64 nodes of 64 heads of 128 over up to 4096 bf16 keys, 248
+// GFLOP, 321 us, 770 TFLOP/s), few rows by memory (40 sequences over up to 8000 e4m3 keys 71 us, 5.0 TB/s), small calls by their chain
+// (8 nodes over 301 keys 9.4 us).
 #pragma once
 #include "prefixattn_kernel.h"
 #include "treeattn_cut.h"
