@@ -8,9 +8,23 @@ using namespace serving;
 
 namespace {
 
-constexpr int64_t kShort = 1024, kLong = 1 << 20;     // keys of a sequence, and bytes of a head's (see plan_of)
+constexpr int64_t kShort = 1024, kShortBytes = 1 << 19, kLong = 1 << 20;      // keys of a sequence, and bytes of a head's (see plan_of)
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Splits of a prefix over `places` workgroups of many rows, `units` of them a split.  Its parts are written and read: each costs what `part_keys`
+// keys do (256 rows of 128 in fp32, written and read by all CUs at once, 13 us).  The time of n splits is that of as many rounds of workgroups as
+// they need, rounds * keys / n, and of their parts, part_keys * n * units / places; of each number of rounds the most splits it holds are
+// looked at, and fewer where parts are dear.  (44 x 16 nodes of 32 heads over 12000 bf16 keys: 88 units; 3 splits need 264 places, and
+// with up to 300 keys of their own 263 us a call, 5 splits 186; 64 x 16 of 40 over 8000 e4m3 266 and 205, 40 x 16 of 32 over 20000 332 and 242.)
+int64_t prefix_splits_of(int64_t keys, int64_t units, int64_t places, int64_t part_keys, int64_t rounds)
+{
+    int64_t best = std::max<int64_t>(1, std::min(places / units, static_cast<int64_t>(sqrt(static_cast<double>(keys * places) / static_cast<double>(part_keys * units)))));
+    const auto cost = [&](int64_t n) { return (n * units + places - 1) / places * keys / n + part_keys * n * units / places; };
+    for (int64_t round = 2; round <= rounds; ++round)
+        if (const int64_t n = round * places / units; n > 0 && cost(n) < cost(best)) best = n;
+    return best;
+}
 
 // Checks a shape and splits its work.  What a sequence may hold at most counts, for its length is known on the device alone.
 int plan_of(const prefixattn_shape* s, Plan* p)
@@ -28,14 +42,16 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // form with more rows a workgroup goes over them tile by tile.  Whole calls of 32 query and 8 key heads of 128, us, so and with more rows:
     //   8 x 16 nodes over 300 bf16 keys 10.8, 17.2      8 x 32 over 300 14.2, 22.7    2 x 16 over 700 11.4, 16.0     16 x 16 over 1000 23.6, 26.3
     //   16 x 32 over 1000 e4m3 29.3, 32.5               4 x 16 over 1500 18.5, 16.3   32 x 16 over 2000 53.8, 45.3   64 x 16 over 500 51.8, 25.6
+    // and of heads of 256, 15 x 4 of 64 heads over 814 43.5, 25.2, 8 x 8 over 900 25.0, 18.5, 4 x 8 of 40 over 276 11.9, 14.4.
     const int64_t units16 = tiles_of(own, FEW) * a.kv_heads * s->batch;
-    if (width <= kShort && units16 <= 2 * kFinishUnits) p->suffix_form = FEW;
+    const int64_t key_bytes = std::max(256, 2 * p->dp * (s->format == KVCACHE_E4M3 ? 1 : 2));
+    if (width <= kShort && width * key_bytes <= kShortBytes && units16 <= 2 * kFinishUnits) p->suffix_form = FEW;
     // A short prefix is seen by each sequence's workgroups before its own keys, in one launch: with few rows by prefixattn.hip's rule, up to twice the
     // bytes where they fill the chip (64 x 4 nodes over 700 and up to 100 bf16 keys 23.4 us, in two launches 29.4, 32 x 4 over 1400 21.0 and 26.3, over
     // 64 x 1400 33.0 either way); with more rows, where that fills the chip, up to 16 keys for each row of a workgroup, for the work is the same and
     // no part of the prefix's is written (64 x 64 nodes of 64 heads over 300 and up to 500 keys 141 us, so 219, over 2000 359 and 436; 64 x 32
     // nodes of 32 heads over 300 43.7 and 60.3, over 2000 112 and 114, over 8000 349 and 304; 64 x 16 over 600 40.8 and 50.9, over 2000 76.5 and 73.6).
-    const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch, key_bytes = std::max(256, 2 * p->dp * (s->format == KVCACHE_E4M3 ? 1 : 2));
+    const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch;
     const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
     const bool together = p->suffix_form != FEW ? width && units >= kFinishUnits && a.prefix_len <= 16 * kFormRows[p->suffix_form]
                           : units >= kFinishUnits ? units * prefix_bytes <= 2 * kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
@@ -58,27 +74,42 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     const int64_t prefix_units = static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, each = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads, suffix_units = each * s->batch;
     auto split_prefix = [&](int64_t n) { a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, n, kMinChunk, &a.prefix_chunk) : 0; };
     const int64_t slots = wanted(p->prefix_form), own_slots = wanted(p->suffix_form);
-    split_prefix(slots);
+    const int64_t part_keys = (p->prefix_form == MANY_256 ? 640 : 320) * all / (static_cast<int64_t>(a.prefix_tiles) * kFormRows[p->prefix_form]) + 1;
+    split_prefix(p->prefix_form == FEW || !prefix ? slots : prefix_units * prefix_splits_of(a.prefix_len, prefix_units, slots, part_keys, 4));
     // Where the sequences fill the chip, a workgroup goes over all of a sequence's keys and joins the prefix's parts: no parts of the sequences'
     // own (64 x 8 nodes over 1000 e4m3 keys 26.2 us in place of 38.7, 64 x 64 over 4096 bf16 338 in place of 465).  So also where one launch is
-    // all there is to few keys (8 nodes over 301 10.2, with two launches 10.8; over 700 13.6 and 11.6).  With few rows, whose parts are small,
+    // all there is to few keys (8 nodes over 301 10.2, with two launches 10.8; over 700 13.6 and 11.6; beside a prefix it is not: 6 x 2 over 4284 and
+    // up to 12 of 256 23.0, joined by the sequences 30.3).  With few rows, whose parts are small,
     // long sequences are cut until there are two workgroups a CU (40 sequences over 8000 e4m3 keys 90.6, cut 70.5; 64 x 2 over 4000 the same).
-    p->finish = suffix && a.prefix_splits <= kFinishSplits &&
-                (suffix_units >= (p->suffix_form == FEW && width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (p->suffix_form == FEW && width <= kShort / 2));
+    // With many rows, whose parts are large, they are cut where that fills places for long: 32 x 16 nodes of 32 heads (256 workgroups in 512 places)
+    // over up to 1500 bf16 keys 34.0 us, cut 39.5, over 2500 50.7 and 48.1, 8000 146 and 112; 48 x 16 over 2500 75.4 and 79.9, 8000 252 and 214; 62 x
+    // 16 over 8000 281 and 279.
+    const bool fills = p->suffix_form != FEW ? suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots
+                                             : suffix_units >= (width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (width <= kShort / 2 && !prefix);
+    p->finish = suffix && a.prefix_splits <= kFinishSplits && fills;
     if (p->finish && p->suffix_form == FEW) p->suffix_form = few(suffix_units);
     if (p->finish && !prefix) p->prefix_form = p->suffix_form;
     if (suffix) {
         a.suffix_splits = 1;
         if (!p->finish) {
-            // As many pieces as there are places, less one for the ends of sequences (1 x 32 nodes over 131072 e4m3 keys 96.8 us with 63 pieces of a
-            // head, 103.6 with 64, 111.5 with 96; 8 x 16 over 8191 34.8 with 62, 37.4 with 64, 45.4 with 128); more of them where many sequences end
-            // (40 over 8000: 76.9 with 62, 70.5 with 192).
-            a.cut_least = p->suffix_form == FEW ? kMinChunk : 2 * kMinChunk;
+            // As many pieces as there are places, less the half piece that a sequence ends with; where that is less than a piece a sequence, for
+            // twice the places.  (With 16 rows or 4 a sequence over bf16 keys, in place of 4 pieces a sequence: 16 x 16 nodes of 32 heads over up
+            // to 4000 37.1 us, so 44.8; 12 x 32 of 40 over 8000 89 and 102; 16 x 4 over 8000 50.3 and 58.6; 12 x 2 of 8 over 20000 e4m3 47.2 and
+            // 60.5.  Heads of 256: 16 x 4 of 64 over 3000 40.1 and 56.1, 28 x 8 over 2000 for twice the places 53, else 61.6.)
+            // The shortest is two turns; heads of 64, whose turns are short, four (2 x 20 of 64 heads over 1142 15.2 us, with two 16.4; 4 x 32 of 256
+            // over 1200 25.6 and 22.6, 1 x 64 of 128 over 2000 22.8 and 20.9).
+            a.cut_least = p->suffix_form == FEW || p->dp > 64 ? kMinChunk : 2 * kMinChunk;
             const int64_t most = std::min<int64_t>((width * s->batch + a.cut_least - 1) / a.cut_least, kMaxSplits - 1);
-            a.cut_parts = static_cast<int32_t>(std::clamp<int64_t>(std::max<int64_t>(own_slots / each - 1, 4 * s->batch), 1, most));
-            if (prefix) {
+            const int64_t places = own_slots / each, ends = 1 + s->batch / 2, pieces = (places - ends >= s->batch ? places : 2 * places) - ends;
+            a.cut_parts = static_cast<int32_t>(std::clamp<int64_t>(std::max<int64_t>(pieces, s->batch), 1, most));
+            if (prefix && p->prefix_form == FEW) {
                 const int64_t own_blocks = std::min<int64_t>(a.cut_parts + s->batch, (width * s->batch + a.cut_least - 1) / a.cut_least) * each;
                 split_prefix(std::max(slots / 2, slots - own_blocks));
+            } else if (prefix) {
+                // The prefix's share of the places, as if sequences were half as long as they may be (17 x 30 nodes of 16 heads over 10062 fp16 keys of 96
+                // and up to 1495 77.8 us, in half the places 93.8; 16 x 16 of 32 over 16000 and 1500 110 and 133, over 2000 and 1500 54.7 in all of them).
+                const int64_t share = 2ll * a.prefix_len * slots / (2ll * a.prefix_len + width);
+                split_prefix(prefix_units * std::min((share + prefix_units - 1) / prefix_units, prefix_splits_of(a.prefix_len, prefix_units, slots, part_keys, 1)));
             }
         }
         // the longest first where not all start at once (32 x 64 nodes over up to 4096 keys 170 us, in their order 214; where all start, 1.5 us are lost)

@@ -140,7 +140,30 @@ CASES = [
     (64, 3, 8, 4, 128, 100, [], 0, 32, "fp16", False),
     (2, 10, 8, 2, 256, 40, [], 0, 8, "bf16", False),
 ]
+SHARED_OUT = [
+    # many sequences, a few of them long: cut although their workgroups nearly fill the chip, alone and beside a prefix
+    (33, 17, 8, 8, 64, 0, [2200 if i % 16 == 3 else (37 * i) % 90 for i in range(33)], 70, 32, "bf16", False),
+    (33, 17, 8, 8, 64, 1500, [2200 if i % 16 == 3 else (37 * i) % 90 for i in range(33)], 70, 32, "fp16", True),
+    (36, 9, 16, 8, 128, 130, [2210 if i == 7 else (31 * i) % 60 for i in range(36)], 35, 64, "bf16", True),
+    # sequences of few keys, of few rows, beside a prefix seen by many rows
+    (3, 15, 1, 1, 256, 2500, [6, 0, 40], 1, 64, "bf16", True),
+    (12, 4, 8, 4, 128, 1300, [(17 * i) % 100 for i in range(12)], 7, 16, "bf16", False),
+    (7, 7, 8, 2, 256, 1000, [(29 * i) % 90 for i in range(7)], 4, 32, "fp16", False),
+    # a prefix in as many splits as rounds of workgroups hold, and in the share of the places that its keys are of all
+    (20, 40, 8, 2, 128, 1100, [(41 * i) % 130 for i in range(20)], 3, 64, "bf16", False),
+    (44, 16, 32, 8, 64, 900, [(13 * i) % 60 for i in range(44)], 3, 32, "bf16", True),
+    (5, 30, 16, 4, 96, 2100, [1400, 3, 0, 77, 600], 30, 64, "fp16", False),
+]
 name = lambda c: "x".join(str(x) for x in c[:6]) + f"_{c[8]}_{c[9]}_{'e4m3' if c[10] else 'same'}"  # noqa: E731
+
+
+@pytest.mark.parametrize("case", SHARED_OUT, ids=name)
+def test_work_that_is_shared_out_against_64_bits(case):
+    c, dtype = build(case, seed=case[0] + case[5], odd=case[0] % 2 == 0)
+    got = call(c, dtype)
+    check(c, dtype, got)
+    again = call(c, dtype)
+    assert torch.equal(again[0].view(torch.uint8), got[0].view(torch.uint8)) and torch.equal(again[1], got[1])
 
 
 @pytest.mark.parametrize("case", CASES, ids=name)
