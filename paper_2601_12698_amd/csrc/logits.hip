@@ -390,7 +390,16 @@ int check(int64_t batch, int32_t nodes, int64_t vocab, int dtype)
 // x 40000 10.0 in place of 9.1, 256 x 50001 23.7 in place of 22.5, 8 x 24 x 100000 fp32 38.2 in place of 33.4, 16 x 8 x 152000 22.9 and 19.5.
 // Of the others, long histories are gone over half as often by 512 threads (8 x 24 x 131072 with up to 16384 32.4 us in place of 33.3, 1 x 64 nodes x
 // 50001 with 30000 18.4 and 23.1), short ones are not worth it (256 x 50001 24.9 in place of 22.4).
-int threads_of(int64_t vocab, int32_t history) { return vocab <= kEach * kManyThreads ? kManyThreads : history >= kLongHistory ? kLongThreads : kThreads; }
+// Rows of up to 16384 tokens have threads enough in 512 or 256, of which more come on a CU: 58 x 11 x 8000 bf16 9.3 us with 256, 13.2 with 512, 15.8 with
+// 1024, 100 x 3 x 2900 9.3, 10.7 and 14.8, 58 x 11 x 16000 15.1 with 512 and 17.4 with 1024, 54 x 8000 with histories of up to 19500 19.0, 14.4 and 14.9,
+// 1 x 8000 8.1, 7.3 and 8.1.  Where 1024 for each row find room at once, short rows are no faster with fewer (1 x 2900 7.9, 7.7 and 6.9).
+int threads_of(int64_t rows, int64_t vocab, int32_t history)
+{
+    const bool many = rows > 256;
+    if (vocab <= kEach * kThreads && many && history < kLongHistory) return kThreads;
+    if (vocab <= kEach * kLongThreads && (vocab > 4096 || many)) return kLongThreads;
+    return vocab <= kEach * kManyThreads ? kManyThreads : history >= kLongHistory ? kLongThreads : kThreads;
+}
 int64_t chunks_of(int64_t vocab, int threads) { return (vocab + kEach * threads - 1) / (kEach * threads); }
 // Partial results of a row: one of each wave, none where one workgroup has the row.
 int64_t partials_of(int64_t vocab, int threads) { return chunks_of(vocab, threads) > 1 ? chunks_of(vocab, threads) * (threads / 64) : 0; }
@@ -447,14 +456,14 @@ int logits_run(const void* logits, int64_t logits_stride, void* out, int64_t out
     a.logits_stride = logits_stride, a.out_stride = out_stride, a.history_stride = l.history_stride, a.allowed_stride = l.allowed_stride;
     a.vocab = static_cast<uint32_t>(vocab), a.nodes = static_cast<uint32_t>(nodes), a.rows = static_cast<uint32_t>(batch * nodes);
     a.biases = static_cast<uint32_t>(l.biases), a.history_width = static_cast<uint32_t>(l.history_width);
-    const int threads = threads_of(vocab, a.history ? l.history_width : 0);
+    const int threads = threads_of(batch * nodes, vocab, a.history ? l.history_width : 0);
     a.chunks = static_cast<uint32_t>(chunks_of(vocab, threads));
     a.partials = static_cast<uint32_t>(partials_of(vocab, threads));
     const bool used = l.biases || (l.penalties && (a.history || l.tree_masks));
     // A tree's rows are shared out until the chip is full twice over, or with one workgroup a CU full; each share takes in the lists anew (8
     // x 24 nodes x 131072 with 256 threads: 52.6 us with 256 workgroups, 35.8 with 512, 33.3 with 1024, 36.7 with 2048).
     const int64_t wanted = threads == kThreads ? 1024 : threads == kLongThreads ? 512 : 256, units = a.chunks * batch;
-    int64_t parts = used ? (wanted + units - 1) / units : nodes;
+    int64_t parts = used ? std::max<int64_t>(1, wanted / units) : nodes;
     if (parts > nodes) parts = nodes;
     a.part_rows = static_cast<uint32_t>((nodes + parts - 1) / parts);
     a.parts = static_cast<uint32_t>((nodes + a.part_rows - 1) / a.part_rows);

@@ -93,6 +93,15 @@ def test_against_the_steps_in_fp32_and_64_bits(case):
     assert torch.equal(alone[0].view(torch.uint8), got[0].view(torch.uint8))
 
 
+@pytest.mark.parametrize("case", [dict(batch=90, nodes=3, vocab=2901, dtype="bf16", width=40, biases=300, masked=True, tree=True),
+                                  dict(batch=260, nodes=1, vocab=500, dtype="fp32", width=9, biases=5), dict(batch=44, nodes=6, vocab=9000, dtype="fp16", width=70, masked=True),
+                                  dict(batch=2, nodes=5, vocab=8192, dtype="bf16", width=9000, biases=1, tree=True), dict(batch=1, nodes=1, vocab=16384, dtype="fp32", width=100),
+                                  dict(batch=100, nodes=3, vocab=4097, dtype="bf16", masked=True)], ids=lambda c: "_".join(str(x) for x in c.values()))
+def test_rows_of_one_workgroup_of_each_size(case):
+    c = build(**case, seed=case["vocab"])
+    check(c, case["dtype"], case["nodes"], call(c, case["dtype"], case["nodes"]))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 def test_strides_unaligned_rows_and_in_place(dtype):
     c = build(3, 2, 9001, dtype, width=50, biases=4, masked=True, tree=True, seed=1)
