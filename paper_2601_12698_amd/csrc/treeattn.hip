@@ -10,6 +10,10 @@ namespace {
 
 constexpr int64_t kShort = 1024, kShortBytes = 1 << 19, kLong = 1 << 20;      // keys of a sequence, and bytes of a head's (see plan_of)
 
+// Up to here a row is joined by several workgroups, each of some of its columns: 15 rows of 256 in 255 parts 20.6 us a call in place of 27.6, 4 of 128
+// 20.7 and 22.9; 384 of 256 40.7 and 41.5, 512 of 256 25.1 in place of 24.1.
+constexpr int64_t kNarrowRows = 256;
+
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Splits of a prefix over `places` workgroups of many rows, `units` of them a split.  Its parts are written and read: each costs what `part_keys`
@@ -36,24 +40,29 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     const int64_t width = s->suffix_width * s->page_size, all = static_cast<int64_t>(s->batch) * s->q_len * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
     p->suffix_form = form_of(own, p->dp);
     p->prefix_form = form_of(all, p->dp);
-    auto wanted = [p](int form) { return form == MANY_256 || (form == MANY_128 && p->dp > 128) ? 256 : 512; };
-    auto few = [](int64_t units) { return units <= kFinishUnits ? FEW_8 : FEW; };
+    auto wanted = [p](int form) { return form == MANY_256 || p->dp > 128 ? 256 : 512; };          // one workgroup a CU, or two
+    // Eight waves of a workgroup, or four where workgroups fill the chip.  Heads of 256 leave room for one workgroup a CU in either case (60 x 3 nodes of
+    // 32 heads over 200 bf16 keys 23.3 us, with four waves 28.5, 64 x 4 over 3000 e4m3 101 and 113; cut into pieces for 256 places, with four waves and for
+    // 512, 4 x 2 over 2000 bf16 16.9 and 22.9, 1 x 3 over 30000 44.9 and 52.3).
+    auto few = [p](int64_t units) { return p->dp > 128 || units <= kFinishUnits ? FEW_8 : FEW; };
     // Sequences of few keys: 16 rows a workgroup, whose waves share the keys, as often as there are rows; it reads the keys as often, but a
     // form with more rows a workgroup goes over them tile by tile.  Whole calls of 32 query and 8 key heads of 128, us, so and with more rows:
     //   8 x 16 nodes over 300 bf16 keys 10.8, 17.2      8 x 32 over 300 14.2, 22.7    2 x 16 over 700 11.4, 16.0     16 x 16 over 1000 23.6, 26.3
     //   16 x 32 over 1000 e4m3 29.3, 32.5               4 x 16 over 1500 18.5, 16.3   32 x 16 over 2000 53.8, 45.3   64 x 16 over 500 51.8, 25.6
-    // and of heads of 256, 15 x 4 of 64 heads over 814 43.5, 25.2, 8 x 8 over 900 25.0, 18.5, 4 x 8 of 40 over 276 11.9, 14.4.
+    // and of heads of 256, 15 x 4 of 64 heads over 814 43.5, 25.2, 8 x 8 over 900 25.0, 18.5, 4 x 8 of 40 over 276 11.9, 14.4;
+    // one a CU: 48 x 14 of 8 over 36 and up to 1 18.8, 10.5, 10 x 24 of 32 over 400 28.7, 23.9, over 900 e4m3 30.9, 37.1.
     const int64_t units16 = tiles_of(own, FEW) * a.kv_heads * s->batch;
     const int64_t key_bytes = std::max(256, 2 * p->dp * (s->format == KVCACHE_E4M3 ? 1 : 2));
-    if (width <= kShort && width * key_bytes <= kShortBytes && units16 <= 2 * kFinishUnits) p->suffix_form = FEW;
+    if (width <= kShort && width * key_bytes <= kShortBytes && units16 <= (p->dp > 128 && width <= kShort / 2 ? 1 : 2) * kFinishUnits) p->suffix_form = FEW;
     // A short prefix is seen by each sequence's workgroups before its own keys, in one launch: with few rows by prefixattn.hip's rule, up to twice the
     // bytes where they fill the chip (64 x 4 nodes over 700 and up to 100 bf16 keys 23.4 us, in two launches 29.4, 32 x 4 over 1400 21.0 and 26.3, over
     // 64 x 1400 33.0 either way); with more rows, where that fills the chip, up to 16 keys for each row of a workgroup, for the work is the same and
     // no part of the prefix's is written (64 x 64 nodes of 64 heads over 300 and up to 500 keys 141 us, so 219, over 2000 359 and 436; 64 x 32
-    // nodes of 32 heads over 300 43.7 and 60.3, over 2000 112 and 114, over 8000 349 and 304; 64 x 16 over 600 40.8 and 50.9, over 2000 76.5 and 73.6).
+    // nodes of 32 heads over 300 43.7 and 60.3, over 2000 112 and 114, over 8000 349 and 304; 64 x 16 over 600 40.8 and 50.9, over 2000 76.5 and 73.6), or where all
+    // keys are few (25 x 40 of 32 heads over 300 and up to 100 25.5 us, in two launches 56).
     const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch;
     const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
-    const bool together = p->suffix_form != FEW ? width && units >= kFinishUnits && a.prefix_len <= 16 * kFormRows[p->suffix_form]
+    const bool together = p->suffix_form != FEW ? width && ((units >= kFinishUnits && a.prefix_len <= 16 * kFormRows[p->suffix_form]) || a.prefix_len + width <= kShort)
                           : units >= kFinishUnits ? units * prefix_bytes <= 2 * kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
     if (a.pages && a.prefix_len && together) {
         if (p->suffix_form == FEW) p->suffix_form = few(units);
@@ -83,8 +92,9 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // long sequences are cut until there are two workgroups a CU (40 sequences over 8000 e4m3 keys 90.6, cut 70.5; 64 x 2 over 4000 the same).
     // With many rows, whose parts are large, they are cut where that fills places for long: 32 x 16 nodes of 32 heads (256 workgroups in 512 places)
     // over up to 1500 bf16 keys 34.0 us, cut 39.5, over 2500 50.7 and 48.1, 8000 146 and 112; 48 x 16 over 2500 75.4 and 79.9, 8000 252 and 214; 62 x
-    // 16 over 8000 281 and 279.
-    const bool fills = p->suffix_form != FEW ? suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots
+    // 16 over 8000 281 and 279; and not where keys are few (38 x 62 of 5 heads over 2 8.7 and 20.9, 17 x 40 of 32 over 400 20.0 and 38.9, 18 x 46 of 16
+    // heads of 64 over 500 12.8 and 20.8).
+    const bool fills = p->suffix_form != FEW ? (width <= kShort && !prefix) || suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots
                                              : suffix_units >= (width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (width <= kShort / 2 && !prefix);
     p->finish = suffix && a.prefix_splits <= kFinishSplits && fills;
     if (p->finish && p->suffix_form == FEW) p->suffix_form = few(suffix_units);
@@ -116,6 +126,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
         a.sorted = p->finish && s->batch <= 64 && suffix_units > own_slots;
         p->suffix_blocks = round_up(a.kv_heads * (p->finish ? static_cast<int64_t>(s->batch) : a.cut_parts + static_cast<int64_t>(s->batch)), 8) * a.suffix_tiles;
     }
+    if (p->dp > 128 && p->prefix_form == FEW) p->suffix_form = p->prefix_form = FEW_8;
     p->prefix_blocks = round_up(static_cast<int64_t>(a.prefix_splits) * a.kv_heads, 8) * a.prefix_tiles;
     // parts of a sequence
     const int64_t parts = static_cast<int64_t>(a.prefix_splits) * s->batch + (a.cut_parts ? a.cut_parts + static_cast<int64_t>(s->batch) : 0);
@@ -170,10 +181,11 @@ int treeattn_run(const void* q, const int64_t* q_strides, const void* k_pages, c
         return ADDRMS_OK;
     }
     if (p.prefix_blocks + p.suffix_blocks) SERVING_HIP_TRY(unit(a, p.prefix_form, p.suffix_form, static_cast<unsigned>(p.prefix_blocks + p.suffix_blocks), s));
-    const bool many = p.rows >= kJoinRows;
-    SERVING_HIP_TRY(launch_kernel(shape->dtype == ADDRMS_FP16 ? (many ? tree_join_kernel<DT_FP16, 1> : tree_join_kernel<DT_FP16, 4>)
-                                                              : (many ? tree_join_kernel<DT_BF16, 1> : tree_join_kernel<DT_BF16, 4>),
-                                  dim3(static_cast<unsigned>(many ? (p.rows + 3) / 4 : p.rows)), dim3(kJoinThreads), s, a));
+    const bool many = p.rows >= kJoinRows, narrow = !many && p.rows <= kNarrowRows && a.d > kJoinColumns;
+    const int64_t blocks = many ? (p.rows + 3) / 4 : narrow ? p.rows * ((a.d + kJoinColumns - 1) / kJoinColumns) : p.rows;
+#define JOIN(DT) (many ? tree_join_kernel<DT, 1, false> : narrow ? tree_join_kernel<DT, 4, true> : tree_join_kernel<DT, 4, false>)
+    SERVING_HIP_TRY(launch_kernel(shape->dtype == ADDRMS_FP16 ? JOIN(DT_FP16) : JOIN(DT_BF16), dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads), s, a));
+#undef JOIN
     return ADDRMS_OK;
 }
 

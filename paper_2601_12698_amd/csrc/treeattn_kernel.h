@@ -24,7 +24,7 @@ template <int DT, int FORMAT, int DP, int WAVES, bool TWO> struct tree_form<DT, 
 // key range stand 8 apart, so that they read it through the same L2 at the same time.
 // TWO: the sequences' workgroups of many rows see the prefix first.  (Those of few rows may, in either case.)
 template <int DT, int FORMAT, int DP, int PREFIX, int SUFFIX, bool TWO>
-__global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW ? 1 : 2)) void tree_kernel(AttnArgs a)
+__global__ __launch_bounds__(threads_of(PREFIX, DP), 2) void tree_kernel(AttnArgs a)
 {
     constexpr int WAVES = threads_of(PREFIX, DP) / 64;          // few rows use all of them, whatever the prefix's form
     typedef typename form<DT, FORMAT, DP, PREFIX, WAVES>::type P;
@@ -97,8 +97,10 @@ __global__ __launch_bounds__(threads_of(PREFIX, DP), (DP > 128 && PREFIX == FEW 
 }
 
 // As prefixattn.hip's: out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, lse = ln 2 (m + log2 of that sum), over the prefix's parts and
-// those of the row's sequence.  WAVES waves join a row, lanes being columns of four elements by groups of parts.
-template <int DT, int WAVES>
+// those of the row's sequence.  WAVES waves join a row, lanes being columns of four elements by groups of parts.  NARROW: a workgroup has
+// kJoinColumns of a row's elements, so that more lanes share its parts.
+constexpr int kJoinColumns = 64;
+template <int DT, int WAVES, bool NARROW>
 __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(AttnArgs a)
 {
     typedef typename elem<DT>::type T;
@@ -108,7 +110,8 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(AttnArgs a)
     __shared__ f32x4 sums[kJoinThreads];
     const int32_t tid = static_cast<int32_t>(threadIdx.x) % THREADS, slot = static_cast<int32_t>(threadIdx.x) / THREADS, wave = tid >> 6;
     const int32_t each = a.q_len * a.q_heads, rows = a.batch * each;
-    const int32_t row = __builtin_amdgcn_readfirstlane(static_cast<int32_t>(blockIdx.x) * ROWS + slot);
+    const int32_t pieces = NARROW ? (a.d + kJoinColumns - 1) / kJoinColumns : 1, block = static_cast<int32_t>(blockIdx.x) / pieces, piece = static_cast<int32_t>(blockIdx.x) - block * pieces;
+    const int32_t row = __builtin_amdgcn_readfirstlane(block * ROWS + slot);
     if (row >= rows) return;                                    // with one wave a row: no barrier follows
     const auto meet = [] {
         if constexpr (WAVES > 1) __syncthreads();
@@ -126,7 +129,8 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(AttnArgs a)
         own = (static_cast<int64_t>(a.prefix_splits) * a.batch + cut.before - seq) * each + row;
     }
     const auto place = [&](int32_t p) { return p < a.prefix_splits ? static_cast<int64_t>(p) * rows + row : own + static_cast<int64_t>(p - a.prefix_splits) * each; };
-    const int32_t cols = a.d / 4, groups = THREADS / cols, grp = tid / cols, col = tid - grp * cols;
+    const int32_t cols = NARROW ? kJoinColumns / 4 : a.d / 4, groups = THREADS / cols, grp = tid / cols, lane_col = tid - grp * cols;
+    const int32_t col = NARROW ? min(lane_col + piece * cols, a.d / 4 - 1) : lane_col;            // lanes beyond the head do as the last one does
     const float* o = at_global<const float>(a.part_o) + 4 * col;
     const int32_t mine = grp < groups && grp < parts ? (parts - grp + groups - 1) / groups : 0;      // parts that this lane adds
     f32x4 first[AHEAD];
@@ -172,7 +176,7 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(AttnArgs a)
     sums[threadIdx.x] = x;
     meet();
     if (grp == 0) {
-        for (int32_t g = 1; g < groups; ++g) x += sums[slot * THREADS + g * cols + col];
+        for (int32_t g = 1; g < groups; ++g) x += sums[slot * THREADS + g * cols + lane_col];
         const float inverse = l == 0.0f ? 0.0f : 1.0f / l;              // no key was seen: zeros
         T4 y;
 #pragma unroll

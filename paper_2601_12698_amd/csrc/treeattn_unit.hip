@@ -16,7 +16,8 @@ hipError_t launch(const AttnArgs& a, unsigned blocks, hipStream_t s)
 hipError_t TREE_UNIT(UNIT_DT, UNIT_FORMAT, UNIT_DP)(const AttnArgs& a, int prefix_form, int suffix_form, unsigned blocks, hipStream_t s)
 {
     if (prefix_form == FEW_8) return launch<FEW_8, FEW_8>(a, blocks, s);
-    if (prefix_form == FEW) return launch<FEW, FEW>(a, blocks, s);
+    if constexpr (UNIT_DP <= 128)
+        if (prefix_form == FEW) return launch<FEW, FEW>(a, blocks, s);
     if (a.inline_len) {
         if constexpr (UNIT_DP <= 128)
             if (suffix_form == MANY_64) return launch<MANY_64, MANY_64, true>(a, blocks, s);

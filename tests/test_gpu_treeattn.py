@@ -149,6 +149,15 @@ SHARED_OUT = [
     (3, 15, 1, 1, 256, 2500, [6, 0, 40], 1, 64, "bf16", True),
     (12, 4, 8, 4, 128, 1300, [(17 * i) % 100 for i in range(12)], 7, 16, "bf16", False),
     (7, 7, 8, 2, 256, 1000, [(29 * i) % 90 for i in range(7)], 4, 32, "fp16", False),
+    # few keys in all, of many rows; rows joined by several workgroups each; heads beyond 128 of few rows
+    (20, 36, 32, 4, 128, 0, [(19 * i) % 200 for i in range(20)], 4, 64, "bf16", False),
+    (20, 30, 16, 2, 64, 90, [(23 * i) % 300 for i in range(20)], 6, 64, "fp16", True),
+    (2, 15, 1, 1, 256, 80, [3000, 1700], 95, 32, "bf16", True),
+    (2, 3, 4, 1, 96, 0, [2500, 60], 80, 32, "fp16", False),
+    (1, 2, 4, 1, 80, 40, [4000], 64, 64, "bf16", True),
+    (3, 4, 8, 2, 256, 20, [1300, 900, 2], 42, 32, "fp16", False),
+    (1, 1, 260, 260, 256, 1100, [20], 1, 32, "bf16", True),
+    (2, 4, 4, 1, 256, 700, [], 0, 32, "bf16", False),
     # a prefix in as many splits as rounds of workgroups hold, and in the share of the places that its keys are of all
     (20, 40, 8, 2, 128, 1100, [(41 * i) % 130 for i in range(20)], 3, 64, "bf16", False),
     (44, 16, 32, 8, 64, 900, [(13 * i) % 60 for i in range(44)], 3, 32, "bf16", True),
