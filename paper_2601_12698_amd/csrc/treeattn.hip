@@ -16,6 +16,8 @@ constexpr int64_t kNarrowRows = 256;
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
+constexpr int64_t kPartKeys = 640;       // that cost as much as a part of 256 rows: below
+
 // Splits of a prefix over `places` workgroups of many rows, `units` of them a split.  Its parts are written and read: each costs what `part_keys`
 // keys do (256 rows of 128 in fp32, written and read by all CUs at once, 13 us).  The time of n splits is that of as many rounds of workgroups as
 // they need, rounds * keys / n, and of their parts, part_keys * n * units / places; of each number of rounds the most splits it holds are
@@ -38,8 +40,14 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     if (p->rows == 0) return ADDRMS_OK;
     AttnArgs& a = p->a;
     const int64_t width = s->suffix_width * s->page_size, all = static_cast<int64_t>(s->batch) * s->q_len * a.group, own = static_cast<int64_t>(s->q_len) * a.group;
-    p->suffix_form = form_of(own, p->dp);
-    p->prefix_form = form_of(all, p->dp);
+    // 128 rows a workgroup where 256 would leave a half without one (40 x 34 nodes of 64 query and 8 key heads over 2000 e4m3 keys 82.6 us in place of 112,
+    // 8 x 64 of 48 over 8000 100 and 117; 12 x 7 of 32 beside a prefix of 8000 bf16 keys 33.9 and 38.1).  A sequence's form is never the larger one.
+    const auto shape_form = [p](int64_t rows) {
+        const int form = form_of(rows, p->dp);
+        return form == MANY_256 && tiles_of(rows, MANY_128) < 2 * tiles_of(rows, MANY_256) ? MANY_128 : form;
+    };
+    p->suffix_form = shape_form(own);
+    p->prefix_form = p->suffix_form == MANY_256 ? form_of(all, p->dp) : shape_form(all);
     auto wanted = [p](int form) { return form == MANY_256 || p->dp > 128 ? 256 : 512; };          // one workgroup a CU, or two
     // Eight waves of a workgroup, or four where workgroups fill the chip.  Heads of 256 leave room for one workgroup a CU in either case (60 x 3 nodes of
     // 32 heads over 200 bf16 keys 23.3 us, with four waves 28.5, 64 x 4 over 3000 e4m3 101 and 113; cut into pieces for 256 places, with four waves and for
@@ -62,7 +70,11 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // keys are few (25 x 40 of 32 heads over 300 and up to 100 25.5 us, in two launches 56).
     const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch;
     const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
-    const bool together = p->suffix_form != FEW ? width && ((units >= kFinishUnits && a.prefix_len <= 16 * kFormRows[p->suffix_form]) || a.prefix_len + width <= kShort)
+    // Also where that leaves places idle for no more than kPartKeys keys (30 x 14 of 32 heads over 900 and up to 300 29.8 us and 41.3, 28 x 60 over 3000 and
+    // 400 e4m3 112 and 156, 60 x 60 of 16 over 3000 and 400 120 and 252; not 10 x 30 of 32, 4 of them key heads, over 1500 and 100, 58 and 38).
+    const int64_t room = wanted(p->suffix_form);
+    const bool idle = (2ll * a.prefix_len + width) * (room - units) > 2 * kPartKeys * room;
+    const bool together = p->suffix_form != FEW ? width && (a.prefix_len + width <= kShort || (a.prefix_len <= 16 * kFormRows[p->suffix_form] && (units >= kFinishUnits || !idle)))
                           : units >= kFinishUnits ? units * prefix_bytes <= 2 * kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
     if (a.pages && a.prefix_len && together) {
         if (p->suffix_form == FEW) p->suffix_form = few(units);
@@ -83,7 +95,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     const int64_t prefix_units = static_cast<int64_t>(a.prefix_tiles) * a.kv_heads, each = static_cast<int64_t>(a.suffix_tiles) * a.kv_heads, suffix_units = each * s->batch;
     auto split_prefix = [&](int64_t n) { a.prefix_splits = prefix ? splits_of(a.prefix_len, prefix_units, n, kMinChunk, &a.prefix_chunk) : 0; };
     const int64_t slots = wanted(p->prefix_form), own_slots = wanted(p->suffix_form);
-    const int64_t part_keys = (p->prefix_form == MANY_256 ? 640 : 320) * all / (static_cast<int64_t>(a.prefix_tiles) * kFormRows[p->prefix_form]) + 1;
+    const int64_t part_keys = (p->prefix_form == MANY_256 ? kPartKeys : kPartKeys / 2) * all / (static_cast<int64_t>(a.prefix_tiles) * kFormRows[p->prefix_form]) + 1;
     split_prefix(p->prefix_form == FEW || !prefix ? slots : prefix_units * prefix_splits_of(a.prefix_len, prefix_units, slots, part_keys, 4));
     // Where the sequences fill the chip, a workgroup goes over all of a sequence's keys and joins the prefix's parts: no parts of the sequences'
     // own (64 x 8 nodes over 1000 e4m3 keys 26.2 us in place of 38.7, 64 x 64 over 4096 bf16 338 in place of 465).  So also where one launch is

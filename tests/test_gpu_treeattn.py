@@ -158,6 +158,10 @@ SHARED_OUT = [
     (3, 4, 8, 2, 256, 20, [1300, 900, 2], 42, 32, "fp16", False),
     (1, 1, 260, 260, 256, 1100, [20], 1, 32, "bf16", True),
     (2, 4, 4, 1, 256, 700, [], 0, 32, "bf16", False),
+    # rows in tiles of 128 where tiles of 256 would leave a half empty; a longer prefix before sequences that nearly fill the chip
+    (6, 52, 10, 2, 128, 0, [(211 * i) % 1400 for i in range(6)], 46, 32, "bf16", True),
+    (2, 28, 10, 1, 128, 1300, [40, 600], 20, 32, "fp16", False),
+    (30, 14, 16, 8, 128, 900, [(11 * i) % 70 for i in range(30)], 10, 32, "bf16", False),
     # a prefix in as many splits as rounds of workgroups hold, and in the share of the places that its keys are of all
     (20, 40, 8, 2, 128, 1100, [(41 * i) % 130 for i in range(20)], 3, 64, "bf16", False),
     (44, 16, 32, 8, 64, 900, [(13 * i) % 60 for i in range(44)], 3, 32, "bf16", True),
