@@ -102,12 +102,14 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // all there is to few keys (8 nodes over 301 10.2, with two launches 10.8; over 700 13.6 and 11.6; beside a prefix it is not: 6 x 2 over 4284 and
     // up to 12 of 256 23.0, joined by the sequences 30.3).  With few rows, whose parts are small,
     // long sequences are cut until there are two workgroups a CU (40 sequences over 8000 e4m3 keys 90.6, cut 70.5; 64 x 2 over 4000 the same).
+    // Beside a prefix they are so where one launch fills places that they alone leave idle (36 x 4 over 8000 and up to 700 bf16 keys 47.6, joined by the
+    // sequences 60.0, 8 x 20 over 4000 and 900 39.6 and 48.5; 64 x 4 over 8000 and 700, which fill the chip, 80 and 70).
     // With many rows, whose parts are large, they are cut where that fills places for long: 32 x 16 nodes of 32 heads (256 workgroups in 512 places)
     // over up to 1500 bf16 keys 34.0 us, cut 39.5, over 2500 50.7 and 48.1, 8000 146 and 112; 48 x 16 over 2500 75.4 and 79.9, 8000 252 and 214; 62 x
     // 16 over 8000 281 and 279; and not where keys are few (38 x 62 of 5 heads over 2 8.7 and 20.9, 17 x 40 of 32 over 400 20.0 and 38.9, 18 x 46 of 16
     // heads of 64 over 500 12.8 and 20.8).
-    const bool fills = p->suffix_form != FEW ? (width <= kShort && !prefix) || suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots
-                                             : suffix_units >= (width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (width <= kShort / 2 && !prefix);
+    const bool fills = p->suffix_form != FEW ? (width <= kShort && !prefix) || (suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots)
+                                             : suffix_units >= (prefix ? own_slots : width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (width <= kShort / 2 && !prefix);
     p->finish = suffix && a.prefix_splits <= kFinishSplits && fills;
     if (p->finish && p->suffix_form == FEW) p->suffix_form = few(suffix_units);
     if (p->finish && !prefix) p->prefix_form = p->suffix_form;
