@@ -66,15 +66,15 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // bytes where they fill the chip (64 x 4 nodes over 700 and up to 100 bf16 keys 23.4 us, in two launches 29.4, 32 x 4 over 1400 21.0 and 26.3, over
     // 64 x 1400 33.0 either way); with more rows, where that fills the chip, up to 16 keys for each row of a workgroup, for the work is the same and
     // no part of the prefix's is written (64 x 64 nodes of 64 heads over 300 and up to 500 keys 141 us, so 219, over 2000 359 and 436; 64 x 32
-    // nodes of 32 heads over 300 43.7 and 60.3, over 2000 112 and 114, over 8000 349 and 304; 64 x 16 over 600 40.8 and 50.9, over 2000 76.5 and 73.6), or where all
-    // keys are few (25 x 40 of 32 heads over 300 and up to 100 25.5 us, in two launches 56).
+    // nodes of 32 heads over 300 43.7 and 60.3, over 2000 112 and 114, over 8000 349 and 304; 64 x 16 over 600 40.8 and 50.9, over 2000 76.5 and 73.6).
     const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch;
     const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
     // Also where that leaves places idle for no more than kPartKeys keys (30 x 14 of 32 heads over 900 and up to 300 29.8 us and 41.3, 28 x 60 over 3000 and
-    // 400 e4m3 112 and 156, 60 x 60 of 16 over 3000 and 400 120 and 252; not 10 x 30 of 32, 4 of them key heads, over 1500 and 100, 58 and 38).
+    // 400 e4m3 112 and 156, 60 x 60 of 16 over 3000 and 400 120 and 252; 25 x 40 over 300 and 100 25.5 and 56; not 10 x 30 of 32, 4 of them key heads, over 1500 and 100,
+    // 58 and 38).
     const int64_t room = wanted(p->suffix_form);
     const bool idle = (2ll * a.prefix_len + width) * (room - units) > 2 * kPartKeys * room;
-    const bool together = p->suffix_form != FEW ? width && (a.prefix_len + width <= kShort || (a.prefix_len <= 16 * kFormRows[p->suffix_form] && (units >= kFinishUnits || !idle)))
+    const bool together = p->suffix_form != FEW ? width && a.prefix_len <= 16 * kFormRows[p->suffix_form] && (units >= kFinishUnits || !idle)
                           : units >= kFinishUnits ? units * prefix_bytes <= 2 * kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
     if (a.pages && a.prefix_len && together) {
         if (p->suffix_form == FEW) p->suffix_form = few(units);
@@ -106,9 +106,13 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // sequences 60.0, 8 x 20 over 4000 and 900 39.6 and 48.5; 64 x 4 over 8000 and 700, which fill the chip, 80 and 70).
     // With many rows, whose parts are large, they are cut where that fills places for long: 32 x 16 nodes of 32 heads (256 workgroups in 512 places)
     // over up to 1500 bf16 keys 34.0 us, cut 39.5, over 2500 50.7 and 48.1, 8000 146 and 112; 48 x 16 over 2500 75.4 and 79.9, 8000 252 and 214; 62 x
-    // 16 over 8000 281 and 279; and not where keys are few (38 x 62 of 5 heads over 2 8.7 and 20.9, 17 x 40 of 32 over 400 20.0 and 38.9, 18 x 46 of 16
-    // heads of 64 over 500 12.8 and 20.8).
-    const bool fills = p->suffix_form != FEW ? (width <= kShort && !prefix) || (suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots)
+    // 16 over 8000 281 and 279.
+    // Fewer workgroups than that are cut where a whole sequence takes longer than a place's share, a launch (400 keys; 800 of heads of 64) and the parts:
+    // 12 x 5 nodes of 40 heads of 256 over 740 fp16 keys 16.5 us, whole 24.5, 17 x 40 of 16 of 128 over 900 25.2 and 32.7, over 420 24.1 and 21.1, 40 x 40 of 16
+    // over 620 38.5 and 25.8, 60 x 30 of 8 of 64 over 800 e4m3 24.9 and 16.2.
+    const int64_t share = std::max<int64_t>(kMinChunk, width * suffix_units / (2 * own_slots));
+    const bool brief = !prefix && width <= (p->dp > 64 ? 400 : 800) + share + ((p->rows * a.d * (width / share + 1)) >> 15);
+    const bool fills = p->suffix_form != FEW ? brief || (suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots)
                                              : suffix_units >= (prefix ? own_slots : width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (width <= kShort / 2 && !prefix);
     p->finish = suffix && a.prefix_splits <= kFinishSplits && fills;
     if (p->finish && p->suffix_form == FEW) p->suffix_form = few(suffix_units);
