@@ -69,12 +69,16 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // nodes of 32 heads over 300 43.7 and 60.3, over 2000 112 and 114, over 8000 349 and 304; 64 x 16 over 600 40.8 and 50.9, over 2000 76.5 and 73.6).
     const int64_t units = tiles_of(own, p->suffix_form) * a.kv_heads * s->batch;
     const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
-    // Also where that leaves places idle for no more than kPartKeys keys (30 x 14 of 32 heads over 900 and up to 300 29.8 us and 41.3, 28 x 60 over 3000 and
-    // 400 e4m3 112 and 156, 60 x 60 of 16 over 3000 and 400 120 and 252; 25 x 40 over 300 and 100 25.5 and 56; not 10 x 30 of 32, 4 of them key heads, over 1500 and 100,
-    // 58 and 38).
-    const int64_t room = wanted(p->suffix_form);
-    const bool idle = (2ll * a.prefix_len + width) * (room - units) > 2 * kPartKeys * room;
-    const bool together = p->suffix_form != FEW ? width && a.prefix_len <= 16 * kFormRows[p->suffix_form] && (units >= kFinishUnits || !idle)
+    // Also where a sequence's keys and the prefix's take no longer than apart (30 x 14 of 32 heads over 900 and up to 300 29.8 us and 41.3, 28 x 60 over 3000
+    // and 400 e4m3 112 and 156, 60 x 60 of 16 over 3000 and 400 120 and 252, 25 x 40 over 300 and 100 25.5 and 56; not 10 x 30 of 32, 4 of them key heads,
+    // over 1500 and 100, 58 and 38).
+    // What cutting costs, in keys that a workgroup goes over: a place's share, a launch (400; 800 of heads of 64; 200 for two kinds of work) and the parts.
+    const auto apart = [p, width](int64_t prefix_len, int64_t units, int64_t places) {
+        const int64_t share = std::max<int64_t>(kMinChunk, (2 * prefix_len + width) * units / (2 * places));
+        return (p->dp > 64 ? 400 : 800) + (prefix_len ? 200 : 0) + share + ((p->rows * p->a.d * ((prefix_len + width) / share + 1)) >> 15);
+    };
+    const bool many_together = width && a.prefix_len <= 16 * kFormRows[p->suffix_form] && (units >= kFinishUnits || a.prefix_len + width <= apart(a.prefix_len, units, wanted(p->suffix_form)));
+    const bool together = p->suffix_form != FEW ? many_together
                           : units >= kFinishUnits ? units * prefix_bytes <= 2 * kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
     if (a.pages && a.prefix_len && together) {
         if (p->suffix_form == FEW) p->suffix_form = few(units);
@@ -107,11 +111,9 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     // With many rows, whose parts are large, they are cut where that fills places for long: 32 x 16 nodes of 32 heads (256 workgroups in 512 places)
     // over up to 1500 bf16 keys 34.0 us, cut 39.5, over 2500 50.7 and 48.1, 8000 146 and 112; 48 x 16 over 2500 75.4 and 79.9, 8000 252 and 214; 62 x
     // 16 over 8000 281 and 279.
-    // Fewer workgroups than that are cut where a whole sequence takes longer than a place's share, a launch (400 keys; 800 of heads of 64) and the parts:
-    // 12 x 5 nodes of 40 heads of 256 over 740 fp16 keys 16.5 us, whole 24.5, 17 x 40 of 16 of 128 over 900 25.2 and 32.7, over 420 24.1 and 21.1, 40 x 40 of 16
-    // over 620 38.5 and 25.8, 60 x 30 of 8 of 64 over 800 e4m3 24.9 and 16.2.
-    const int64_t share = std::max<int64_t>(kMinChunk, width * suffix_units / (2 * own_slots));
-    const bool brief = !prefix && width <= (p->dp > 64 ? 400 : 800) + share + ((p->rows * a.d * (width / share + 1)) >> 15);
+    // Fewer workgroups than that are cut where a whole sequence takes longer: 12 x 5 nodes of 40 heads of 256 over 740 fp16 keys 16.5 us, whole 24.5, 17 x 40
+    // of 16 of 128 over 900 25.2 and 32.7, over 420 24.1 and 21.1, 40 x 40 of 16 over 620 38.5 and 25.8, 60 x 30 of 8 of 64 over 800 e4m3 24.9 and 16.2.
+    const bool brief = !prefix && width <= apart(0, suffix_units, own_slots);
     const bool fills = p->suffix_form != FEW ? brief || (suffix_units >= kFinishUnits && width * (own_slots - suffix_units) <= kShort * own_slots)
                                              : suffix_units >= (prefix ? own_slots : width * key_bytes > kLong ? 2 * kFinishUnits : kFinishUnits) || (width <= kShort / 2 && !prefix);
     p->finish = suffix && a.prefix_splits <= kFinishSplits && fills;
