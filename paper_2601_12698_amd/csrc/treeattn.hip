@@ -71,7 +71,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     const int64_t prefix_bytes = a.prefix_len * key_bytes, chain = prefix_bytes + width * key_bytes;
     // Also where a sequence's keys and the prefix's take no longer than apart (30 x 14 of 32 heads over 900 and up to 300 29.8 us and 41.3, 28 x 60 over 3000
     // and 400 e4m3 112 and 156, 60 x 60 of 16 over 3000 and 400 120 and 252, 25 x 40 over 300 and 100 25.5 and 56; not 10 x 30 of 32, 4 of them key heads,
-    // over 1500 and 100, 58 and 38).
+    // over 1500 and 100, 58 and 38, nor 1 x 19 of 8 over 19 and 1072, 39 and 16).
     // What cutting costs, in keys that a workgroup goes over: a place's share, a launch (400; 800 of heads of 64; 200 for two kinds of work) and the parts.
     const auto apart = [p, width](int64_t prefix_len, int64_t units, int64_t places) {
         const int64_t share = std::max<int64_t>(kMinChunk, (2 * prefix_len + width) * units / (2 * places));
@@ -79,7 +79,7 @@ int plan_of(const prefixattn_shape* s, Plan* p)
     };
     const bool many_together = width && a.prefix_len <= 16 * kFormRows[p->suffix_form] && (units >= kFinishUnits || a.prefix_len + width <= apart(a.prefix_len, units, wanted(p->suffix_form)));
     const bool together = p->suffix_form != FEW ? many_together
-                          : units >= kFinishUnits ? units * prefix_bytes <= 2 * kInlineBytes : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
+                          : units >= kFinishUnits ? prefix_bytes <= 2 * kInlineBytes / units : chain <= (units >= kFinishUnits / 2 ? 2 * kInlineChain : kInlineChain);
     if (a.pages && a.prefix_len && together) {
         if (p->suffix_form == FEW) p->suffix_form = few(units);
         p->prefix_form = p->suffix_form;
