@@ -127,7 +127,7 @@ def _compile_serving(force: bool, jobs: int, hdrs) -> list:
     """Objects of the operators around a decode step's attention, and of those that check drafted tokens.  The attention kernels are
     one unit for each element type, cache format and padded head size, so that they compile side by side."""
     deps = [*hdrs, os.path.join(CSRC, "serving_internal.h"), *(os.path.join(ROOT, "include", h) for h in SERVING_HEADERS)]
-    attn = [os.path.join(CSRC, f) for f in ("prefixattn_kernel.h", "prefixattn_args.h", "prefixattn_plan.h", "treeattn_kernel.h", "treeattn_cut.h")]
+    attn = [os.path.join(CSRC, f) for f in ("prefixattn_kernel.h", "prefixattn_args.h", "prefixattn_plan.h", "treeattn_kernel.h", "treeattn_cut.h", "treeattn_plan.h")]
     units = [(n, n[:-4], [], []) for n in ("rotary.hip", "kvcache.hip", "kvmove.hip", "treeaccept.hip", "logits.hip")]
     units += [("prefixattn.hip", "prefixattn", [], attn), ("treeattn.hip", "treeattn", [], attn)]
     for op in ("prefixattn", "treeattn"):

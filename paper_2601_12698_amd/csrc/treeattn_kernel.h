@@ -99,7 +99,6 @@ __global__ __launch_bounds__(threads_of(PREFIX, DP), 2) void tree_kernel(AttnArg
 // As prefixattn.hip's: out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p, lse = ln 2 (m + log2 of that sum), over the prefix's parts and
 // those of the row's sequence.  WAVES waves join a row, lanes being columns of four elements by groups of parts.  NARROW: a workgroup has
 // kJoinColumns of a row's elements, so that more lanes share its parts.
-constexpr int kJoinColumns = 64;
 template <int DT, int WAVES, bool NARROW>
 __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(AttnArgs a)
 {
