@@ -80,7 +80,7 @@ inline int tree_plan_of(const prefixattn_shape* s, Plan* p)
         a.inline_len = a.prefix_len;
         a.suffix_splits = 1;
         a.suffix_tiles = static_cast<int32_t>(tiles_of(own, p->suffix_form));
-        a.sorted = s->batch <= 64 && units > wanted(p->suffix_form);
+        a.sorted = width && s->batch <= 64 && units > wanted(p->suffix_form);      // without keys of their own there are no lengths to look at
         p->suffix_blocks = round_up(a.kv_heads * static_cast<int64_t>(s->batch), 8) * a.suffix_tiles;
         return fits(*p);
     }

@@ -137,6 +137,12 @@ def check(c, dtype, got, want):
     assert ((got[1].double() - lse).abs()[fine] <= (x + 2.0 ** -18 + 2.0 ** -22 * lse.abs())[fine]).all()
 
 
+@pytest.mark.parametrize("case", P.WITHOUT_OWN, ids=P.name)
+def test_a_prefix_alone_seen_by_many_workgroups(case):
+    c = build(case)
+    check(c, case[8], call(c, case[8]), exact(c))
+
+
 @pytest.mark.parametrize("case", P.CASES, ids=P.name)
 def test_every_way_against_64_bits(case):
     batch, nodes, hq, hk, d, prefix, width, page, dtype, quantised = case
@@ -159,7 +165,7 @@ def test_every_way_against_64_bits(case):
             if j >= width * page or (n == "k" and b % 4):
                 continue
             x = strange[n + "_pages"]
-            place = int(c["suffix_pages"][b, j // page]), head % hk, j % page, e
+            place = int(c["suffix_pages"][b, j // page]), head % hk, j % page, e % d
             if quantised:
                 x.view(torch.uint8)[place] = 0x7f
             else:

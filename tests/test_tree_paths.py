@@ -47,3 +47,12 @@ def test_every_form_of_a_workgroup_has_a_case(driver):
         assert {(dp, p, s, "cut") for i, p in enumerate(many) for s in ("few", *many[:i + 1])} <= ran
         assert {(dp, p, "-", "none") for p in (*many, few)} <= ran and {(dp, few, few, "cut"), (dp, "-", "few8", "whole")} <= ran
         assert {w[2] for w in ran if w[0] == dp and w[1] in many and w[3] == "whole"} >= {many[0], many[-1]}
+
+
+def test_sequences_without_keys_have_no_order(driver):
+    """Lengths are not there then: a call that sorted by them would read at address 0."""
+    shapes = [c[:6] + (0,) + c[7:] for c in some_shapes(20000, 2)] + P.WITHOUT_OWN
+    plans = [p for p in P.plans_of(driver, shapes) if p]
+    assert len(plans) > 15000 and all(p[5] == "0" and p[3] in ("inline", "none") for p in plans)
+    ordered = [p for p in P.plans_of(driver, [c[:6] + (1,) + c[7:] for c in P.WITHOUT_OWN])]
+    assert all(p[3] == "inline" and p[5] == "1" for p in ordered)

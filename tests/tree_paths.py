@@ -95,13 +95,22 @@ def build_driver(folder):
     return exe
 
 
-def ways_of(driver, cases):
-    """For each case what the driver says of it, without the number of splits and the order of the sequences; None where there is nothing to do
-    or the shape is refused."""
+def plans_of(driver, cases):
+    """For each case what the driver says of it, None where there is nothing to do or the shape is refused."""
     lines = "".join(f"{b} {n} {hq} {hk} {d} {page} {pages_of(c)} {prefix} {width} {int(dtype == 'fp16')} {int(quantised)}\n"
                     for c in cases for b, n, hq, hk, d, prefix, width, page, dtype, quantised in (c,))
     r = subprocess.run([driver], input=lines, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0, r.stdout[-4000:]
     got = [line.split() for line in r.stdout.splitlines()]
     assert len(got) == len(cases)
-    return [(int(f[1]), f[2], f[3], f[4], f[7]) if len(f) == 8 else None for f in got]
+    return [f[1:] if len(f) == 8 else None for f in got]
+
+
+def ways_of(driver, cases):
+    """The same without the number of splits and the order of the sequences."""
+    return [p and (int(p[0]), *p[1:4], p[6]) for p in plans_of(driver, cases)]
+
+
+# without keys of their own, and with lists and lengths that are not there, in more workgroups than the chip has places
+WITHOUT_OWN = [(20, 3, 80, 16, 256, 2, 0, 32, "fp16", True), (60, 20, 64, 16, 64, 40, 0, 16, "bf16", False), (40, 10, 240, 16, 128, 5, 0, 8, "fp16", False),
+               (40, 24, 224, 16, 112, 100, 0, 4, "bf16", True), (50, 9, 16, 16, 192, 33, 0, 64, "bf16", True)]
