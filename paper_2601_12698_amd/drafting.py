@@ -22,7 +22,7 @@ from ctypes import POINTER, Structure, byref, c_float, c_int, c_int32, c_int64, 
 from . import binding as B
 from . import serving as S
 from .binding import AddrmsError, AddrmsLibraryMissing  # noqa: F401  (what the calls raise)
-from .serving import PrefixAttnShape, _cache, _dtype, _heads, _on_device, _whole
+from .serving import PrefixAttnShape, _cache, _dtype, _heads, _on_device, _tables, _whole
 
 MAX_NODES, MAX_MOVED, MAX_BIASES, MAX_HISTORY = 64, 256, 1023, 1048575
 
@@ -117,13 +117,12 @@ def treeattn_run(q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_len
     dt = _dtype(dtype)
     if q.dim() != 3 or masks.dim() != 2:
         raise ValueError("q must be [batch * nodes, heads, d] and masks [batch, nodes]")
+    _tables(prefix_pages, prefix_len, suffix_pages, suffix_lens)
     rows, hq, _ = q.shape
     batch, nodes = masks.shape
     fmt, pages, hk, page, d, ptrs = _cache(k_pages, v_pages, k_scale, v_scale, dt, q.device)
     qs = _heads("q", q, dt, (batch * nodes, hq, d))
     seen = _whole("masks", masks, "int64", (batch, nodes), q.device)
-    if prefix_len < 0:
-        raise ValueError("prefix_len must be >= 0")
     width = 0
     tables = [None, None, None]
     if prefix_len:
@@ -235,11 +234,13 @@ def treeaccept_run(chosen, tokens, masks, suffix_pages, suffix_lens, page_size: 
             return
     if masks.dim() != 2 or path.dim() != 2:
         raise ValueError("masks must be [batch, nodes] and path [batch, depth]")
+    if (from_slots is None) != (to_slots is None):
+        raise ValueError("from_slots and to_slots are given together")
+    if from_slots is not None and (suffix_pages is None or suffix_lens is None):
+        raise ValueError("from_slots have suffix_pages and suffix_lens")
     (batch, nodes), depth, dev = masks.shape, path.shape[1], masks.device
     ptrs = [_whole("chosen", chosen, "int32", (batch, nodes), dev), _whole("tokens", tokens, "int32", (batch, nodes), dev),
             _whole("masks", masks, "int64", (batch, nodes))]
-    if (from_slots is None) != (to_slots is None):
-        raise ValueError("from_slots and to_slots are given together")
     width = 0
     if from_slots is None:
         ptrs += [None, None]

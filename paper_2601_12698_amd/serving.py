@@ -138,6 +138,16 @@ def _cache(k_pages, v_pages, k_scale, v_scale, dt: int, device):
     return (KVCACHE_E4M3 if quantised else KVCACHE_SAME), pages, heads, page, d, ptrs
 
 
+def _tables(prefix_pages, prefix_len: int, suffix_pages, suffix_lens) -> None:
+    """What a prefix and suffixes come with."""
+    if prefix_len < 0:
+        raise ValueError("prefix_len must be >= 0")
+    if prefix_len and prefix_pages is None:
+        raise ValueError(f"a prefix of {prefix_len} keys has prefix_pages")
+    if suffix_pages is not None and suffix_pages.numel() and suffix_lens is None:
+        raise ValueError("suffix_pages have suffix_lens")
+
+
 # ---- rotary positions (include/rotary.h) ------------------------------------------------------------------------
 
 def rotary_algorithmic_bytes(tokens: int, heads: int, d: int, axes: int, dtype) -> int:
@@ -271,12 +281,11 @@ def prefixattn_run(q, k_pages, v_pages, k_scale, v_scale, prefix_pages, prefix_l
     dt = _dtype(dtype)
     if q.dim() != 3 or q_len < 1 or q.shape[0] % q_len:
         raise ValueError(f"q must be [batch * q_len, heads, d], and q_len={q_len} at least 1")
+    _tables(prefix_pages, prefix_len, suffix_pages, suffix_lens)
     rows, hq, d = q.shape
     batch = rows // q_len
     fmt, pages, hk, page, _, ptrs = _cache(k_pages, v_pages, k_scale, v_scale, dt, q.device)
     qs = _heads("q", q, dt, (rows, hq, k_pages.shape[3]))
-    if prefix_len < 0:
-        raise ValueError("prefix_len must be >= 0")
     first = width = 0
     tables = [None, None, None]
     if prefix_len:

@@ -213,3 +213,19 @@ def test_the_kernels_take_no_scratch_memory():
                 seen += 1
                 assert r["scratch"] == 0, (kernel, r)
     assert seen > 50
+
+
+def test_what_is_left_out_is_named():
+    """A prefix without pages, pages without lengths: the binding's own words, not those of a None that is asked for its shape."""
+    x = torch.zeros(6, 2, 64, dtype=torch.bfloat16)
+    pages, masks, i32 = torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16), torch.ones(2, 3, dtype=torch.int64), torch.zeros(2, 3, dtype=torch.int32)
+    for run, more in ((D.treeattn_run, (masks,)), (S.prefixattn_run, ())):
+        with pytest.raises(ValueError, match="has prefix_pages"):
+            run(x, pages, pages, None, None, None, 5, i32, i32[:, 0], *more, x, None, 0.1, "bf16")
+        with pytest.raises(ValueError, match="have suffix_lens"):
+            run(x, pages, pages, None, None, None, 0, i32, None, *more, x, None, 0.1, "bf16")
+        with pytest.raises(ValueError, match="prefix_len must be"):
+            run(x, pages, pages, None, None, None, -1, None, None, *more, x, None, 0.1, "bf16")
+    for missing in ((None, i32[:, 0]), (i32, None)):
+        with pytest.raises(ValueError, match="have suffix_pages and suffix_lens"):
+            D.treeaccept_run(i32, i32, masks, *missing, 16, 3, i32, i32[:, 0], i32[:, 0], masks, masks)
