@@ -65,14 +65,15 @@ class Layer:
         x = self.embed.clone()
         B.addrms_run(x, torch.zeros_like(x), self.norm, EPS, VOCAB, HIDDEN, "bf16")
         self.guesses = torch.cat([(part @ self.head).topk(3, 1).indices for part in x.split(4000)])
-        # what a step works on: certain tokens but for the last (the prompt's first), lengths, the last one
-        self.prompt_tokens = torch.randint(0, VOCAB, (prompt + batch,), generator=g, device=device)
+        # the prompt, and the token that each sequence begins with, as if drawn after it: node 0 of the first tree, which counts as made
+        tokens = torch.randint(0, VOCAB, (prompt + batch,), generator=g, device=device)
+        self.prompt_tokens, self.last = tokens[:prompt], tokens[prompt:].to(torch.int32)
+        # what a step works on besides: the certain tokens before node 0, and lengths
         self.history = torch.zeros((batch, prompt + room + 1), dtype=torch.int32, device=device)
-        self.history[:, :prompt] = self.prompt_tokens[:prompt]
+        self.history[:, :prompt] = self.prompt_tokens
         self.history_lens = torch.full((batch,), prompt, dtype=torch.int32, device=device)
         self.prompt_lens, self.suffix_lens = self.history_lens.clone(), torch.zeros(batch, dtype=torch.int32, device=device)
         self.penalties = torch.tensor([[1.1, 0.2, 0.1]] * batch, device=device)
-        self.last = self.prompt_tokens[prompt:].to(torch.int32)
         rows = batch * self.nodes
         self.tokens, self.best = torch.zeros((batch, self.nodes), dtype=torch.int32, device=device), torch.zeros((batch, self.nodes), dtype=torch.int32, device=device)
         self.path, self.count = torch.zeros((batch, DEPTH), dtype=torch.int32, device=device), torch.zeros(batch, dtype=torch.int32, device=device)
@@ -96,7 +97,7 @@ class Layer:
     def prefill(self):
         """The prompt's keys and values go into the pages all share."""
         n = self.prompt
-        x, _ = self.embedded(self.prompt_tokens[:n])
+        x, _ = self.embedded(self.prompt_tokens)
         q, k, v = self.heads(x)
         token = torch.arange(n, device=self.device)
         S.rotary_run(q, k, q, k, token[None], self.inv_freq, self.pair_axis, "bf16")

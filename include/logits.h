@@ -5,7 +5,8 @@
  * Sequence b has `nodes` rows, b * nodes ... b * nodes + nodes - 1: one for decoding, or the nodes of a tree of drafted
  * tokens.  For row i of sequence b and token t, with x the logit, every step rounded to fp32:
  *     made   = how often t is among the sequence's tokens history[b][prompt_lens[b] ... history_lens[b] - 1], plus how
- *              many of the nodes that bits of tree_masks[b][i] name have the token t
+ *              many of the nodes that bits of tree_masks[b][i] name have the token t (node 0, the last token that
+ *              is certain, is one of them: the history ends before it, or it counts twice)
  *     met    = made > 0, or t is among history[b][0 ... prompt_lens[b] - 1]
  *     z = x                                      with (r, f, p) = penalties[b]:
  *     z = z > 0 ? z / r : z * r                  if met
@@ -35,7 +36,7 @@ extern "C" {
 typedef struct logits_lists {
     const int32_t* history;         /* [batch], rows of history_width tokens, history_stride apart        */
     const int32_t* history_lens;    /* [batch]; below 0 counts as 0, beyond history_width as history_width */
-    const int32_t* prompt_lens;     /* [batch], as history_lens; NULL: no prompts                         */
+    const int32_t* prompt_lens;     /* [batch], as history_lens, and beyond these as these; NULL: no prompts */
     const float* penalties;         /* [batch][3]: r, f, p; NULL: 1, 0, 0, and history is not looked at   */
     const int32_t* bias_tokens;     /* [batch][biases]                                                    */
     const float* bias_values;       /* [batch][biases]                                                    */

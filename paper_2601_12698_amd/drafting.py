@@ -168,8 +168,9 @@ def logits_run(logits, out, best, dtype, nodes: int = 1, history=None, history_l
     """logits [batch * nodes, vocab] (rows any distance apart) -> out (as logits, or logits itself; None: not written) and best
     (int32 [batch * nodes], None: not looked for).  history int32 [batch, width], history_lens and prompt_lens int32 [batch]; penalties
     fp32 [batch, 3] (repetition, frequency, presence); bias_tokens int32 and bias_values fp32 [batch, n]; allowed int32 [batch * nodes,
-    ceil(vocab / 32) or more], bit t % 32 of word t / 32; tree_tokens int32 and tree_masks int64 [batch, nodes].  ``workspace``: bytes on
-    the device, as many as logits_workspace_bytes says; without one the call takes it from torch's allocator, on the current stream."""
+    ceil(vocab / 32) or more], bit t % 32 of word t / 32; tree_tokens int32 and tree_masks int64 [batch, nodes], whose history ends before
+    node 0's token.  ``workspace``: bytes on the device, as many as logits_workspace_bytes says; without one the call takes it from torch's
+    allocator, on the current stream (with best on a stream of its own it brings one, of no bytes where none are needed)."""
     if stream is None and (B._torch_facts or B._torch()) and (native := _fast()) is not None:
         st = native.logits_run(logits, out, best, dtype, nodes, history, history_lens, prompt_lens, penalties, bias_tokens, bias_values, allowed,
                                tree_tokens, tree_masks, workspace)
