@@ -1,4 +1,4 @@
-// What rotary.hip, kvcache.hip and prefixattn.hip share: element types, reductions over a few lanes, argument checks.
+// What the operators around a decode step and those that check drafted tokens share: element types, reductions over a few lanes, argument checks.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
