@@ -229,3 +229,14 @@ def test_what_is_left_out_is_named():
     for missing in ((None, i32[:, 0]), (i32, None)):
         with pytest.raises(ValueError, match="have suffix_pages and suffix_lens"):
             D.treeaccept_run(i32, i32, masks, *missing, 16, 3, i32, i32[:, 0], i32[:, 0], masks, masks)
+
+
+def test_logits_workspace_is_that_of_the_longer_of_two_forms():
+    """8 bytes of each wave of a row's workgroups, where one of 1024 threads with 32 tokens each does not hold the row: 256 or 512 threads then, which of
+    them goes by the histories, which the workspace is not told."""
+    for vocab in (1, 8192, 32768):
+        assert D.logits_workspace_bytes(3, 4, vocab, "bf16") == 0
+    for vocab in (32769, 40960, 49152, 49153, 152000, 1 << 24):
+        partials = max(-(-vocab // (32 * t)) * (t // 64) for t in (256, 512))
+        assert D.logits_workspace_bytes(3, 4, vocab, "fp32") == 8 * 12 * partials
+    assert D.logits_workspace_bytes(1, 1, 40960, "bf16") == 8 * 24 and D.logits_workspace_bytes(1, 1, 40959, "fp16") == 8 * 24      # 5 of 4 waves, 3 of 8

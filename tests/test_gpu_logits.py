@@ -218,6 +218,17 @@ def test_the_workspace_is_as_long_as_it_says():
     assert (room[n:] == 0xff).all()
 
 
+@pytest.mark.parametrize("width", [0, 70, 8191, 8192])
+@pytest.mark.parametrize("vocab", [32769, 40000, 100003])
+def test_the_workspace_is_long_enough_for_either_form_of_long_rows(vocab, width):
+    """Histories from 8192 tokens on are gone over by workgroups of 512 threads, shorter ones by 256: other numbers of partial results."""
+    c = build(2, 1, vocab, "bf16", width=width, biases=3, seed=vocab + width)
+    n = drafting.logits_workspace_bytes(2, 1, vocab, "bf16")
+    room = torch.full((n + 4096,), 0xa5, dtype=torch.uint8, device="cuda")
+    check(c, "bf16", 1, call(c, "bf16", 1, workspace=room[:n]))
+    assert (room[n:] == 0xa5).all()
+
+
 def test_on_another_stream_and_in_a_graph():
     c = build(3, 4, 20011, "bf16", width=100, biases=20, masked=True, tree=True, seed=5)
     dev = {n: x.cuda() for n, x in c.items()}
