@@ -17,7 +17,8 @@
  *   from_slots[b][k], to_slots[b][k]   slots of the key of the path's k-th node, which lies at
  *                    position suffix_lens[b] + path[b][k] of its row of pages, and of position
  *                    suffix_lens[b] + k, where it belongs: what kvmove.h moves in groups of `depth`
- *                    tokens.  Both -1 where it is there already, beyond the path, and where either
+ *                    tokens (of up to its KVMOVE_MAX_TOKENS; a path has TREE_MAX_NODES at most).
+ *                    Both -1 where it is there already, beyond the path, and where either
  *                    position is beyond the row of pages or on a page outside the cache
  *
  * Status codes, pointer kinds and error text as in addrms.h.
